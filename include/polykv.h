@@ -250,6 +250,118 @@ int pool_attend(const polykv_pool* pool, const void* Q_dev, void* out_dev,
 int pool_attend_static(const polykv_pool* pool, const void* Q_dev, void* out_dev,
                        const polykv_attend_params* params, void* stream);
 
+/* ---- Private continuations in pages, and drafted tokens -------------------------------------------------------
+ *
+ * pool_attend takes an agent's continuation as dense tensors whose lengths are host numbers, of 64 agents at most.  The
+ * calls below keep the continuations of any number of agents in pages of a common store, with block tables and lengths
+ * on the device (a captured graph sees them as they are when it is replayed), and serve steps in which every agent has
+ * several drafted tokens that form a tree: a step is
+ *   polykv_pages_resize   room for the drafts: block tables and the slots of the new tokens
+ *   polykv_tree_masks     which drafts a draft sees, and its depth, from the tree's parents
+ *   polykv_pages_write    the drafts' keys and values into their slots (layer by layer, or all layers)
+ *   pool_attend_tree      attention of the drafts over the shared pool, the agent's own tokens and the drafts they see
+ *   polykv_pages_accept   the path that the model agrees with; its keys and values move to where they stay
+ *   polykv_pages_resize   back to the accepted lengths: pages that are no longer needed are free again
+ * An agent's drafts are the last tokens of its continuation: with lengths[a] tokens in its pages and counts[a] drafts,
+ * token lengths[a] - counts[a] + i is draft i.  A drafted token per agent (nodes = 1) is plain decoding.
+ *
+ * The struct describes the caller's buffers and is read during a call only.  What lies in device memory cannot be
+ * checked by the host: lengths outside [0, max_blocks * page_tokens] and counts outside [0, nodes] are taken as the
+ * nearest bound, a page number outside [0, pages) as a page that is not there (its tokens are neither written nor
+ * attended), a parent that is no earlier draft as none.  Calls that write the buffers and calls that read them must be
+ * ordered by the caller (same stream, or events). */
+enum {
+    POLYKV_MAX_PAGED_AGENTS = 4096,
+    POLYKV_MAX_TREE_NODES = 256
+};
+typedef struct {
+    int layers, kv_heads, head_dim; /* head_dim 64, 128 or 256; layers * kv_heads <= 65535                      */
+    int pages;                      /* pages of a layer                                                         */
+    int page_tokens;                /* tokens of a page, a multiple of 8; pages * page_tokens <= 2^30 and
+                                       pages * page_tokens * kv_heads < 2^31                                    */
+    int agents;                     /* 1 .. POLYKV_MAX_PAGED_AGENTS                                             */
+    int max_blocks;                 /* pages an agent can have; max_blocks * page_tokens <= 2^30                */
+    int dtype;                      /* POLYKV_F16 or POLYKV_BF16                                                */
+    void* K_dev;                    /* [layers, pages, kv_heads, page_tokens, head_dim], 16-byte aligned        */
+    void* V_dev;
+    int32_t* table_dev;             /* [agents, max_blocks]: the pages of an agent's tokens, in order           */
+    int32_t* lengths_dev;           /* [agents]: tokens in an agent's pages                                     */
+    int32_t* free_dev;              /* [pages]: ring of the free pages' numbers (polykv_pages_resize only)      */
+    int32_t* free_state_dev;        /* [2]: place of the first free page in the ring, and how many there are    */
+} polykv_pages;
+
+/* Block tables and slot maps from lengths: agent a's continuation becomes targets_dev[a] tokens long.  With
+ * have = ceil(lengths[a] / page_tokens) and want = ceil(targets[a] / page_tokens),
+ *   want > have  pages are taken from the front of the ring, in the order of the agents, into table[a][have .. want);
+ *                an agent whose pages are not there -- counting those that the agents before it ask for -- gets none and
+ *                keeps its length, and so do agents behind it that need pages;
+ *   want < have  pages table[a][want .. have) go behind the ring's last, in the order of the agents, and their entries
+ *                become -1; they are there to be taken from the next call on.
+ * A target outside [0, max_blocks * page_tokens] leaves the agent as it is.  lengths, table, free and free_state are
+ * updated.  slots_dev (NULL: not wanted) receives the places of the tokens that the agents grew by, agent after agent:
+ * entry offsets[a] + i belongs to token (old length) + i of agent a and is page * page_tokens + token % page_tokens;
+ * entries behind the last one are -1.  If there are more than `slots` tokens, those past that have no entry.
+ * offsets_dev (NULL: not wanted): int32 [agents + 1]. */
+int polykv_pages_resize(const polykv_pages* pages, const int32_t* targets_dev, int32_t* slots_dev, int slots,
+                        int32_t* offsets_dev, void* stream);
+
+/* Keys and values of `tokens` tokens into the pages of layers [layer_begin, layer_end): vector (layer, token t, head) is
+ * at element layer * layer_stride + t * token_stride + head * head_stride of K_dev / V_dev (the same strides for both)
+ * and goes to slot slots_dev[t]; a slot outside [0, pages * page_tokens) is skipped.  in_dtype: the pages' type, or
+ * POLYKV_F32 (rounded once, to nearest even).  K_dev and V_dev 16-byte aligned, strides >= 0 and multiples of 16 bytes.
+ * Of two tokens with one slot, either may be what stays (element by element). */
+int polykv_pages_write(const polykv_pages* pages, const void* K_dev, const void* V_dev, int in_dtype, int tokens,
+                       int64_t layer_stride, int64_t token_stride, int64_t head_stride, const int32_t* slots_dev,
+                       int layer_begin, int layer_end, void* stream);
+
+/* Trees of drafts: parents_dev int32 [agents, nodes], parents[a][i] an earlier draft of the agent or -1.
+ * mask_dev uint64 [agents, nodes, ceil(nodes / 64)]: bit j % 64 of word j / 64 of draft i is set iff j is i or one of
+ * its ancestors.  depth_dev (NULL: not wanted) int32 [agents, nodes]: the number of its ancestors.  Both are 0 for
+ * drafts from counts_dev[a] on (counts_dev NULL: every agent has `nodes` drafts).  nodes <= POLYKV_MAX_TREE_NODES. */
+int polykv_tree_masks(const int32_t* parents_dev, const int32_t* counts_dev, int agents, int nodes, uint64_t* mask_dev,
+                      int32_t* depth_dev, void* stream);
+
+typedef struct {
+    int nodes;        /* drafts per agent and head in Q, 1 .. POLYKV_MAX_TREE_NODES                    */
+    int q_heads;      /* as in polykv_attend_params, and so are the next seven                        */
+    int layer_begin;
+    int layer_end;
+    float scale;
+    int kernel;       /* of the pool's part                                                           */
+    int splits;       /* token-range splits of the pool's part                                        */
+    int key_precision;
+    int page_splits;  /* token-range splits of the pages' part; 0 = choose automatically              */
+    const int32_t* counts_dev;  /* [agents] drafts of each agent; NULL: `nodes`, as far as its length goes      */
+    const uint64_t* mask_dev;   /* [agents, nodes, ceil(nodes / 64)]: the drafts that a draft sees, any set of
+                                   them; NULL: itself and all before it                                         */
+    void* workspace_dev;        /* 256-byte aligned                                                   */
+    size_t workspace_bytes;     /* >= pool_attend_tree_workspace()                                    */
+} polykv_tree_params;
+
+/* Scratch bytes pool_attend_tree needs for these parameters (workspace fields, counts_dev and mask_dev are ignored). */
+size_t pool_attend_tree_workspace(const polykv_pool* pool, const polykv_pages* pages, const polykv_tree_params* params);
+
+/* Q_dev: [layer_end - layer_begin, agents, nodes, q_heads, head_dim] of the pages' type; out_dev: the same shape and
+ * type (fp32 results rounded once, to nearest even).  Draft i of agent a attends the pool's tokens (pool NULL: there is
+ * none), the agent's tokens before its drafts, and those of its drafts that its mask names.  Rows from counts[a] on
+ * attend the pool alone; a row that sees nothing gets zeros.  The pool's head_dim, layers and kv_heads must be the pages'.
+ * A token that a draft does not see has no effect on it, whatever its vectors hold; a draft that sees a drafted token
+ * with a NaN or infinite value gets NaN.  As in pool_attend, matrix-core kernels round probabilities to fp16 (two bfloat16
+ * terms for bfloat16 pages), and bfloat16 queries of a call with a pool must stay below 65504. */
+int pool_attend_tree(const polykv_pool* pool, const polykv_pages* pages, const void* Q_dev, void* out_dev,
+                     const polykv_tree_params* params, void* stream);
+
+/* The drafts that the model agrees with.  tokens_dev, following_dev, parents_dev int32 [agents, nodes]: the drafted
+ * tokens, what the model puts after each of them, and the trees.  Draft 0, which the model itself has chosen, is
+ * accepted; after an accepted draft i, the first draft c with parent i and tokens[c] == following[i] is, until there is
+ * none.  counts_dev as above.  The accepted drafts' keys and values move, in all layers, to the tokens right behind those
+ * before the drafts.  Outputs, all int32: path_dev [agents, nodes] the accepted drafts, -1 behind them; accepted_dev
+ * [agents] how many; next_dev [agents] what the model puts after the last of them (-1 if there is none); kept_dev
+ * [agents] the length with the accepted drafts, the target for polykv_pages_resize.  lengths are not changed. */
+int polykv_pages_accept(const polykv_pages* pages, const int32_t* tokens_dev, const int32_t* following_dev,
+                        const int32_t* parents_dev, const int32_t* counts_dev, int nodes, int32_t* path_dev,
+                        int32_t* accepted_dev, int32_t* next_dev, int32_t* kept_dev, void* stream);
+
 /* The value codebook the library uses: 8 ascending centroids and the 7 decision thresholds
  * (midpoints), as fp32 (section "TurboQuant", Lloyd-Max quantization).  Host call. */
 void polykv_codebook(float* centroids8, float* thresholds7);

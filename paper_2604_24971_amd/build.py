@@ -10,7 +10,8 @@ from concurrent.futures import ThreadPoolExecutor
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libpolykv.so")
-SOURCES = ["polykv_api.hip", "polykv_codec.hip", "polykv_attend.hip", "polykv_attend_mfma.hip"]
+SOURCES = ["polykv_api.hip", "polykv_codec.hip", "polykv_attend.hip", "polykv_attend_mfma.hip",
+           "polykv_pages.hip", "polykv_tree.hip", "polykv_tree_api.hip"]
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
     # packed-fp32 VALU forms stay off on these machines
@@ -173,7 +174,7 @@ def build_library(verbose: bool = True, extra_flags=()) -> str:
             return "\n".join(l for l in log.splitlines() if "kernel-resource-usage" not in l)
         return _run(cmd)
 
-    with ThreadPoolExecutor(max_workers=4) as ex:
+    with ThreadPoolExecutor(max_workers=6) as ex:
         logs = list(ex.map(compile_one, range(len(SOURCES))))
     logs.append(_run([hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", *objs, "-o", LIB]))
     if verbose:

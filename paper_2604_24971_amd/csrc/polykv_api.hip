@@ -58,7 +58,7 @@ template <int D> static int tile_bytes_of(int vc, int kc) {
 
 // Resolve every choice pool_attend makes from the pool shape and the caller's parameters, so that
 // pool_attend_workspace() and pool_attend() agree by construction.
-static int make_plan(const polykv_pool* pool, const polykv_attend_params* prm, AttendPlan* plan) {
+int make_plan(const polykv_pool* pool, const polykv_attend_params* prm, AttendPlan* plan) {
     if (pool == nullptr || prm == nullptr) {
         set_error("pool_attend: NULL pool or params");
         return POLYKV_EINVAL;
@@ -283,6 +283,28 @@ static int make_plan(const polykv_pool* pool, const polykv_attend_params* prm, A
     return POLYKV_OK;
 }
 
+int check_readable(const polykv_pool* pool, const char* who) {
+    if (pool == nullptr) {
+        set_error("%s: pool is NULL", who);
+        return POLYKV_EINVAL;
+    }
+    if (pool->storage == nullptr) {
+        set_error("%s: no storage bound", who);
+        return POLYKV_ESTATE;
+    }
+    if (pool->length == 0) {
+        set_error("%s: pool has not been encoded", who);
+        return POLYKV_ESTATE;
+    }
+    return POLYKV_OK;
+}
+
+int hip_result(hipError_t e, const char* who) {
+    if (e == hipSuccess) return POLYKV_OK;
+    set_error("%s: HIP error %d (%s)", who, (int)e, hipGetErrorString(e));
+    return POLYKV_EHIP;
+}
+
 }  // namespace polykv
 
 using namespace polykv;
@@ -402,28 +424,6 @@ int pool_bind(polykv_pool* pool, void* dev_storage, size_t bytes) {
     pool->storage = dev_storage;
     pool->length = 0;
     return POLYKV_OK;
-}
-
-static int check_readable(const polykv_pool* pool, const char* who) {
-    if (pool == nullptr) {
-        set_error("%s: pool is NULL", who);
-        return POLYKV_EINVAL;
-    }
-    if (pool->storage == nullptr) {
-        set_error("%s: no storage bound", who);
-        return POLYKV_ESTATE;
-    }
-    if (pool->length == 0) {
-        set_error("%s: pool has not been encoded", who);
-        return POLYKV_ESTATE;
-    }
-    return POLYKV_OK;
-}
-
-static int hip_result(hipError_t e, const char* who) {
-    if (e == hipSuccess) return POLYKV_OK;
-    set_error("%s: HIP error %d (%s)", who, (int)e, hipGetErrorString(e));
-    return POLYKV_EHIP;
 }
 
 static int encode_range(polykv_pool* pool, const void* K_dev, const void* V_dev, int in_dtype, int begin, int count,

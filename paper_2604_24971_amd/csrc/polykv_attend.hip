@@ -420,6 +420,7 @@ hipError_t launch_attend(const polykv_pool* pool, const AttendPlan& plan, const 
         launch_main_kernel(kern, grid, dim3(256), 0, s, storage, (const __half*)Q, ws_ml, ws_o, plan);
         if ((err = hipGetLastError()) != hipSuccess) return err;
     }
+    if (plan.partials_only) return hipSuccess;
     const long nrows = (long)units * plan.R;
     dim3 mgrid((unsigned)((nrows + 3) / 4));
     launch_kernel(plan.D == 128 ? attend_merge_kernel<128> : plan.D == 64 ? attend_merge_kernel<64> : attend_merge_kernel<256>, mgrid,

@@ -1032,7 +1032,7 @@ bool matrix_kernel_supports(int head_dim, int value_codec) { return head_dim != 
 // Query rows per workgroup: 64 (32 at head_dim 256, where 64 rows' accumulators alone would fill the registers).
 int matrix_kernel_block_rows(int head_dim) { return head_dim == 256 ? 32 : 64; }
 
-bool matrix_kernel_direct(const AttendPlan& plan) { return plan.nsplit == 1; }
+bool matrix_kernel_direct(const AttendPlan& plan) { return plan.nsplit == 1 && !plan.partials_only; }
 
 int matrix_kernel_row_tiles(const AttendPlan& plan) { return plan.D != 256 && plan.R > 32 && plan.block_rows == 64 ? 2 : 1; }
 

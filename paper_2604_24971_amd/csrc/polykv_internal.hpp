@@ -64,6 +64,7 @@ struct AttendPlan {
     int references;              // matrix-core kernel: tiles from whose maxima a wave takes a reference of its rows (>= 1)
     float raise_sum;             // ... and the sum of a tile's probabilities beyond which a row moves its reference (<= 2^15)
     int own_rows;                // 1: the waves of a workgroup have rows of their own, 0: they share them
+    int partials_only;           // 1: the call ends with the pool's partials in the workspace
     int has_tails, tail_capacity, tail_causal;
     int io_bf16;                 // 1: Q and the tails are bfloat16, 0: fp16
     int key_fp16;                // 1: scores over the dequantized keys rounded to fp16 (POLYKV_KEY_PRECISION_FP16)
@@ -85,6 +86,10 @@ hipError_t launch_encode(const polykv_pool* p, const void* K, const void* V, int
 hipError_t launch_decode(const polykv_pool* p, void* K_out, void* V_out, int dtype, int layer_begin, int layer_end,
                          hipStream_t s);
 hipError_t launch_export(const polykv_pool* p, void* kc, void* ks, void* vp, void* vs, hipStream_t s);
+// Resolves every choice of a pool_attend call and validates its parameters; the reason of a refusal is in the error text.
+int make_plan(const polykv_pool* pool, const polykv_attend_params* prm, AttendPlan* plan);
+int check_readable(const polykv_pool* pool, const char* who);
+int hip_result(hipError_t e, const char* who);
 hipError_t launch_attend(const polykv_pool* p, const AttendPlan& plan, const void* Q, void* out,
                          const TailPtrs* tails, void* workspace, hipStream_t s);
 

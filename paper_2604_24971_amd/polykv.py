@@ -22,6 +22,7 @@ VALUE_BITS = {0: 3, 1: 3, 2: 8, 3: 2, 4: 2, 5: 4, 6: 4}
 KEYS_Q8_BLOCK32, KEYS_Q8_TENSOR = 0, 1
 MAX_TAIL_AGENTS = 64
 STATIC_WORKSPACE_BYTES = 32 << 20
+MAX_PAGED_AGENTS, MAX_TREE_NODES = 4096, 256
 
 
 class PolyKVError(RuntimeError):
@@ -45,6 +46,19 @@ class AttendParams(C.Structure):
 class AttendChoice(C.Structure):
     _fields_ = [(n, C.c_int) for n in ("kernel", "splits", "block_rows", "own_rows", "references", "tails_in_pool_launch")] + \
         [("grid", C.c_int * 3)]
+
+
+class PagesDesc(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("layers", "kv_heads", "head_dim", "pages", "page_tokens", "agents", "max_blocks", "dtype")] + \
+        [(n, C.c_void_p) for n in ("K_dev", "V_dev", "table_dev", "lengths_dev", "free_dev", "free_state_dev")]
+
+
+class TreeParams(C.Structure):
+    _fields_ = [
+        ("nodes", C.c_int), ("q_heads", C.c_int), ("layer_begin", C.c_int), ("layer_end", C.c_int), ("scale", C.c_float),
+        ("kernel", C.c_int), ("splits", C.c_int), ("key_precision", C.c_int), ("page_splits", C.c_int),
+        ("counts_dev", C.c_void_p), ("mask_dev", C.c_void_p), ("workspace_dev", C.c_void_p), ("workspace_bytes", C.c_size_t),
+    ]
 
 
 def _load():
@@ -93,6 +107,19 @@ def _load():
     lib.pool_attend.restype = ip
     lib.pool_attend_static.argtypes = [vp, vp, vp, C.POINTER(AttendParams), vp]
     lib.pool_attend_static.restype = ip
+    pp, tp, i64 = C.POINTER(PagesDesc), C.POINTER(TreeParams), C.c_int64
+    lib.polykv_pages_resize.argtypes = [pp, vp, vp, ip, vp, vp]
+    lib.polykv_pages_resize.restype = ip
+    lib.polykv_pages_write.argtypes = [pp, vp, vp, ip, ip, i64, i64, i64, vp, ip, ip, vp]
+    lib.polykv_pages_write.restype = ip
+    lib.polykv_tree_masks.argtypes = [vp, vp, ip, ip, vp, vp, vp]
+    lib.polykv_tree_masks.restype = ip
+    lib.pool_attend_tree_workspace.argtypes = [vp, pp, tp]
+    lib.pool_attend_tree_workspace.restype = sz
+    lib.pool_attend_tree.argtypes = [vp, pp, vp, vp, tp, vp]
+    lib.pool_attend_tree.restype = ip
+    lib.polykv_pages_accept.argtypes = [pp, vp, vp, vp, vp, ip, vp, vp, vp, vp, vp]
+    lib.polykv_pages_accept.restype = ip
     lib.polykv_codebook.argtypes = [C.POINTER(C.c_float), C.POINTER(C.c_float)]
     lib.polykv_codebook.restype = None
     lib.polykv_codebook_bits.argtypes = [ip, C.POINTER(C.c_float), C.POINTER(C.c_float)]
@@ -371,3 +398,222 @@ class Pool:
         _check(lib.pool_attend_static(self._h, _dev_ptr(Q, Q.dtype, "Q"), _dev_ptr(out, torch.float32, "out"),
                                       C.byref(p), _stream_ptr(stream)))
         return out
+
+    # pool_attend_tree(Q[drafts], out): the pool, the agents' pages and the drafts in them
+    def attend_tree(self, Q: torch.Tensor, pages: "Pages", out: torch.Tensor | None = None, *, kernel=KERNEL_AUTO, splits=0,
+                    key_precision=KEY_PRECISION_EXACT, **kw):
+        """Attention of every agent's drafted tokens over this pool, then the agent's tokens in `pages` and the drafts
+        among them that a draft sees; the further arguments are Pages.attend_tree()'s."""
+        if self.storage is not None and self.storage.device != pages.device:
+            raise ValueError("the pool is on %s, the pages on %s" % (self.storage.device, pages.device))
+        return pages._attend_tree(self._h, Q, out, kernel=kernel, splits=splits, key_precision=key_precision, **kw)
+
+
+class _OnDevice:
+    """Calls act on the current device and on streams of it; objects on another one switch to it for the call."""
+
+    def __init__(self, device: torch.device):
+        self.index = device.index if device.index is not None else 0
+        self.guard = None
+
+    def __enter__(self):
+        if torch.cuda.current_device() != self.index:
+            self.guard = torch.cuda.device(self.index)
+            self.guard.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            guard, self.guard = self.guard, None
+            guard.__exit__(*exc)
+
+
+def _new(shape, dtype, device, stream=None):
+    """A tensor from the memory of the stream that the call runs on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _ints(t: torch.Tensor, shape, device, what: str) -> int:
+    if t.dtype is torch.int32 and t.shape == shape and t.device == device and t.is_contiguous():
+        return t.data_ptr()
+    raise TypeError("%s must be a contiguous int32 tensor of shape %s on %s" % (what, tuple(shape), device))
+
+
+def tree_masks(parents: torch.Tensor, counts: torch.Tensor | None = None, mask: torch.Tensor | None = None,
+               depth: torch.Tensor | None = None, stream=None):
+    """Trees of drafted tokens: parents int32 [agents, nodes], an earlier draft of the same agent or -1; counts int32
+    [agents], the drafts of each agent (None: all).  Returns (mask, depth): mask int64 [agents, nodes, ceil(nodes / 64)],
+    whose bit j % 64 of word j / 64 says that a draft sees draft j (itself and its ancestors), and depth int32 [agents,
+    nodes], the number of a draft's ancestors -- how far its position is from the first draft's."""
+    if parents.dim() != 2 or not parents.is_cuda:
+        raise TypeError("parents must be a CUDA tensor [agents, nodes]")
+    agents, nodes = parents.shape
+    device = parents.device
+    words = (agents, nodes, (nodes + 63) // 64)
+    with _OnDevice(device):
+        if mask is None:
+            mask = _new(words, torch.int64, device, stream)
+        elif mask.dtype is not torch.int64 or mask.shape != words or mask.device != device or not mask.is_contiguous():
+            raise TypeError("mask must be a contiguous int64 tensor of shape %s on %s" % (words, device))
+        if depth is None:
+            depth = _new((agents, nodes), torch.int32, device, stream)
+        _check(lib.polykv_tree_masks(_ints(parents, parents.shape, device, "parents"),
+                                     _ints(counts, (agents,), device, "counts") if counts is not None else None, agents, nodes,
+                                     mask.data_ptr(), _ints(depth, parents.shape, device, "depth"), _stream_ptr(stream)))
+    return mask, depth
+
+
+class Pages:
+    """Private continuations of `agents` agents in pages of a common store, the counterpart of Tails for any number of
+    agents, lengths on the device and several drafted tokens a step.
+
+      K, V        [layers, pages, kv_heads, page_tokens, head_dim], float16 or bfloat16
+      table       int32 [agents, max_blocks]: the pages of an agent's tokens, in order
+      lengths     int32 [agents]: tokens in an agent's pages, drafts included
+      free, free_state   the ring of free pages, and its first place and how many there are
+
+    Agents start empty and all pages free.  The tensors are the caller's to read, and to write between calls (their
+    storage has to stay)."""
+
+    def __init__(self, layers: int, kv_heads: int, head_dim: int, pages: int, agents: int, max_blocks: int, page_tokens: int = 16,
+                 dtype=torch.float16, device="cuda:0"):
+        if dtype not in (torch.float16, torch.bfloat16):
+            raise TypeError("pages must be float16 or bfloat16")
+        self.layers, self.kv_heads, self.head_dim = layers, kv_heads, head_dim
+        self.pages, self.page_tokens, self.agents, self.max_blocks, self.dtype = pages, page_tokens, agents, max_blocks, dtype
+        device = torch.device(device)
+        self.device = torch.device(device.type, device.index if device.index is not None else 0)
+        shape = (layers, pages, kv_heads, page_tokens, head_dim)
+        self.K = torch.empty(shape, dtype=dtype, device=self.device)
+        self.V = torch.empty(shape, dtype=dtype, device=self.device)
+        self.table = torch.full((agents, max_blocks), -1, dtype=torch.int32, device=self.device)
+        self.lengths = torch.zeros((agents,), dtype=torch.int32, device=self.device)
+        self.free = torch.arange(pages, dtype=torch.int32, device=self.device)
+        self.free_state = torch.tensor([0, pages], dtype=torch.int32, device=self.device)
+        self._desc = PagesDesc(layers, kv_heads, head_dim, pages, page_tokens, agents, max_blocks, _DTYPES[dtype],
+                               *(t.data_ptr() for t in (self.K, self.V, self.table, self.lengths, self.free, self.free_state)))
+        self._ref = C.byref(self._desc)
+        self._workspaces = {}   # stream handle -> cached attend_tree workspace
+
+    # polykv_pages_resize(targets, slots, offsets)
+    def resize(self, targets: torch.Tensor, slots: torch.Tensor | None = None, offsets: torch.Tensor | None = None, stream=None):
+        """Agent a's continuation becomes targets[a] tokens long: pages are taken for it or given back.  An agent for which
+        there are no pages, or whose target is out of range, keeps its length.  `slots` (int32, any length) receives the
+        places of the tokens that agents grew by, for write(), agent after agent, and -1 behind them; `offsets` (int32
+        [agents + 1]) where each agent's begin."""
+        if slots is not None:
+            n = slots.numel()
+            slots = _ints(slots, (n,), self.device, "slots")
+        else:
+            n = 0
+        with _OnDevice(self.device):
+            _check(lib.polykv_pages_resize(self._ref, _ints(targets, (self.agents,), self.device, "targets"), slots, n,
+                                           _ints(offsets, (self.agents + 1,), self.device, "offsets") if offsets is not None else None,
+                                           _stream_ptr(stream)))
+
+    # polykv_pages_write(K, V, slots)
+    def write(self, K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, layer_begin=0, layer_end=None, stream=None):
+        """Keys and values [layers of the range, tokens, kv_heads, head_dim] (the pages' dtype or float32; heads' elements
+        contiguous, any other strides of whole 16 bytes, the same for both) into the slots of their tokens."""
+        layer_end = self.layers if layer_end is None else layer_end
+        if K.dim() != 4 or K.shape != V.shape or K.shape[0] != layer_end - layer_begin or \
+                K.shape[2] != self.kv_heads or K.shape[3] != self.head_dim:
+            raise ValueError("K and V must be [%d, tokens, %d, %d]" % (layer_end - layer_begin, self.kv_heads, self.head_dim))
+        if K.dtype not in (self.dtype, torch.float32) or V.dtype is not K.dtype or K.device != self.device or V.device != self.device:
+            raise TypeError("K and V must be %s or float32 tensors on %s" % (self.dtype, self.device))
+        strides = K.stride()
+        if strides[3] != 1 or V.stride() != strides:
+            raise ValueError("K and V must have the same strides, 1 along head_dim")
+        with _OnDevice(self.device):
+            _check(lib.polykv_pages_write(self._ref, K.data_ptr(), V.data_ptr(), _DTYPES[K.dtype], K.shape[1], strides[0], strides[1],
+                                          strides[2], _ints(slots, (K.shape[1],), self.device, "slots"), layer_begin, layer_end,
+                                          _stream_ptr(stream)))
+
+    # pool_attend_tree(NULL, Q[drafts], out)
+    def attend_tree(self, Q: torch.Tensor, out: torch.Tensor | None = None, **kw):
+        """Attention of every agent's drafted tokens (the last counts[a] of its lengths[a] tokens) over the tokens before
+        them and the drafts that a draft's mask names.  Q [layers of the range, agents, nodes, q_heads, head_dim] of the
+        pages' dtype; the result has its shape and dtype.  counts int32 [agents] (None: `nodes` for every agent); mask int64
+        [agents, nodes, ceil(nodes / 64)] as tree_masks() makes it (None: a draft sees itself and all before it).  Rows
+        of drafts that an agent does not have see no private token."""
+        return self._attend_tree(None, Q, out, **kw)
+
+    def _attend_tree(self, pool, Q, out, *, counts=None, mask=None, layer_begin=0, layer_end=None, scale=None, kernel=KERNEL_AUTO,
+                     splits=0, page_splits=0, key_precision=KEY_PRECISION_EXACT, workspace=None, stream=None):
+        device = self.device
+        p = self._tree_params(Q, layer_begin, layer_end, scale, kernel, splits, page_splits, key_precision)
+        if Q.device != device:
+            raise ValueError("Q is on %s, the pages on %s" % (Q.device, device))
+        if counts is not None:
+            p.counts_dev = _ints(counts, (self.agents,), device, "counts")
+        if mask is not None:
+            words = (self.agents, p.nodes, (p.nodes + 63) // 64)
+            if mask.dtype is not torch.int64 or mask.shape != words or mask.device != device or not mask.is_contiguous():
+                raise TypeError("mask must be a contiguous int64 tensor of shape %s on %s" % (words, device))
+            p.mask_dev = mask.data_ptr()
+        with _OnDevice(device):
+            sp = _stream_ptr(stream)
+            ref = C.byref(p)
+            if out is None:
+                out = _new(Q.shape, self.dtype, device, stream)
+            elif out.shape != Q.shape or out.device != device:
+                raise ValueError("out must have Q's shape %s on %s" % (tuple(Q.shape), device))
+            q_ptr, out_ptr = _dev_ptr(Q, self.dtype, "Q"), _dev_ptr(out, self.dtype, "out")
+            # One cached workspace per stream: calls on different streams may overlap and must not share one.  A call that is
+            # being captured gets one of its own from the graph's memory: graphs may be replayed on any streams.
+            capturing = workspace is None and torch.cuda.is_current_stream_capturing()
+            ws = workspace if workspace is not None else None if capturing else self._workspaces.get(sp)
+            if ws is not None:
+                p.workspace_dev, p.workspace_bytes = _dev_ptr(ws, torch.uint8, "workspace"), ws.numel()
+                rc = lib.pool_attend_tree(pool, self._ref, q_ptr, out_ptr, ref, sp)
+                if rc != ENOMEM or workspace is not None:
+                    _check(rc)
+                    return out
+            need = lib.pool_attend_tree_workspace(pool, self._ref, ref)
+            if need:
+                ws = _new((need,), torch.uint8, device, stream)
+                if not capturing:
+                    self._workspaces[sp] = ws
+                p.workspace_dev, p.workspace_bytes = ws.data_ptr(), need
+            _check(lib.pool_attend_tree(pool, self._ref, q_ptr, out_ptr, ref, sp))
+            return out
+
+    def _tree_params(self, Q, layer_begin, layer_end, scale, kernel, splits, page_splits, key_precision):
+        layer_end = self.layers if layer_end is None else layer_end
+        if Q.dim() != 5:
+            raise ValueError("Q must be [layers_selected, agents, nodes, q_heads, head_dim]")
+        n, agents, nodes, q_heads, d = Q.shape
+        if n != layer_end - layer_begin or agents != self.agents or d != self.head_dim:
+            raise ValueError("Q shape %s does not match the layer range, %d agents and head_dim %d" % (tuple(Q.shape), self.agents, self.head_dim))
+        return TreeParams(nodes, q_heads, layer_begin, layer_end, float(scale or 0.0), kernel, splits, key_precision, page_splits)
+
+    def attend_tree_workspace_bytes(self, Q, pool: "Pool | None" = None, *, layer_begin=0, layer_end=None, kernel=KERNEL_AUTO, splits=0,
+                                    page_splits=0):
+        """Scratch that attend_tree(Q) needs (with a pool: pool.attend_tree(Q, pages)); 0: none."""
+        p = self._tree_params(Q, layer_begin, layer_end, None, kernel, splits, page_splits, KEY_PRECISION_EXACT)
+        return lib.pool_attend_tree_workspace(pool._h if pool is not None else None, self._ref, C.byref(p))
+
+    # polykv_pages_accept(tokens, following, parents)
+    def accept(self, tokens: torch.Tensor, following: torch.Tensor, parents: torch.Tensor, counts: torch.Tensor | None = None,
+               stream=None):
+        """The drafts that the model agrees with: int32 [agents, nodes] the drafted tokens, what the model puts after each
+        of them, and the trees.  Draft 0 is accepted; after an accepted draft the first of its children whose token is what
+        the model puts there.  Their keys and values move to right behind the tokens before the drafts, in all layers.
+        Returns int32 tensors: path [agents, nodes] (-1 behind the accepted drafts), accepted [agents] (how many), following
+        [agents] (the model's token after the last of them) and kept [agents] (the lengths with them, for resize())."""
+        device = self.device
+        if tokens.dim() != 2 or tokens.shape[0] != self.agents:
+            raise ValueError("tokens must be [agents, nodes]")
+        shape = tokens.shape
+        with _OnDevice(device):
+            path = _new(shape, torch.int32, device, stream)
+            # (one tensor each: they outlive each other)
+            accepted, after, kept = (_new((self.agents,), torch.int32, device, stream) for _ in range(3))
+            _check(lib.polykv_pages_accept(self._ref, _ints(tokens, shape, device, "tokens"), _ints(following, shape, device, "following"),
+                                           _ints(parents, shape, device, "parents"),
+                                           _ints(counts, (self.agents,), device, "counts") if counts is not None else None, shape[1],
+                                           path.data_ptr(), accepted.data_ptr(), after.data_ptr(), kept.data_ptr(), _stream_ptr(stream)))
+        return path, accepted, after, kept

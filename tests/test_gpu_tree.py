@@ -1,0 +1,549 @@
+"""Drafted decoding over continuations in pages, against plain 64-bit implementations (tree_util): block tables, writes, masks,
+attention with and without a pool, acceptance, and a step of all of them, eager and in graphs."""
+import numpy as np
+import pytest
+import torch
+
+import tree_util as U
+from paper_2604_24971_amd import workloads as W
+
+pytestmark = pytest.mark.gpu
+F16, BF16 = torch.float16, torch.bfloat16
+
+
+def _pk():
+    from paper_2604_24971_amd import polykv as pk
+    return pk
+
+
+def dev(x, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(x))
+    return (t.to(dtype) if dtype is not None else t).cuda()
+
+
+def rounded(x, dtype):
+    """float64 values as the dtype holds them."""
+    return torch.from_numpy(np.asarray(x, np.float64)).to(dtype).double().numpy()
+
+
+class Setup:
+    """Pages with the agents' tokens scattered over them; whatever no agent holds is NaN."""
+
+    def __init__(self, rng, lengths, d, H=2, P=16, L=1, dtype=F16, kscale=1.0, MB=None, NP=None):
+        pk = _pk()
+        self.lengths, self.P, self.d, self.dtype = np.array(lengths, np.int32), P, d, dtype
+        MB = MB or max(1, -(-max(lengths) // P) + 1)
+        self.table, pages = U.scattered(rng, lengths, P, MB)
+        self.K = np.full((L, pages, H, P, d), np.nan)
+        self.V = np.full((L, pages, H, P, d), np.nan)
+        for a, n in enumerate(lengths):
+            for t in range(n):
+                at = (slice(None), self.table[a, t // P], slice(None), t % P)
+                self.K[at] = rng.standard_normal((L, H, d)) * kscale
+                self.V[at] = rng.standard_normal((L, H, d))
+        self.K, self.V = rounded(self.K, dtype), rounded(self.V, dtype)
+        self.pages = pk.Pages(L, H, d, pages, len(lengths), MB, page_tokens=P, dtype=dtype)
+        self.load()
+
+    def load(self):
+        self.pages.K.copy_(dev(self.K, self.dtype))
+        self.pages.V.copy_(dev(self.V, self.dtype))
+        self.pages.table.copy_(dev(self.table))
+        self.pages.lengths.copy_(dev(self.lengths))
+
+    def check(self, got, Q, counts, seen, pool=None, **kw):
+        out, mag, big = U.attend(Q, self.K, self.V, self.table, self.lengths, counts, seen, pool, **kw)
+        vmax = max(np.nanmax(np.abs(self.V), initial=0.0), np.abs(pool[1]).max() if pool is not None else 0.0)
+        tokens = int(self.lengths.max()) + (pool[0].shape[2] if pool is not None else 0)
+        tol = U.bound(out, mag, big, self.d, self.dtype, tokens, vmax, pool is not None)
+        err = np.abs(got.double().cpu().numpy() - out)
+        assert np.isfinite(err).all(), "not finite at %s" % (np.argwhere(~np.isfinite(err))[0],)
+        assert (err <= tol).all(), "off by %g, %g allowed, at %s" % (err[err > tol].max(), tol[err > tol].min(), np.argwhere(err > tol)[0])
+
+
+LENGTHS = [0, 1, 2, 7, 8, 9, 31, 32, 33, 63, 65, 96, 127, 128, 129, 161, 300]
+
+
+def _pool(rng, L, H, d, T, dtype, **kw):
+    pk = _pk()
+    K = dev(0.3 * rng.standard_normal((L, H, T, d)), dtype)
+    V = dev(rng.standard_normal((L, H, T, d)), dtype)
+    pool = pk.Pool(L, H, d, T, **kw).bind()
+    pool.encode(K, V)
+    Kh, Vh = pool.decode(torch.float32)
+    return pool, (Kh.double().cpu().numpy(), Vh.double().cpu().numpy())
+
+
+@pytest.mark.parametrize("d,group,nodes,P,dtype", [
+    (64, 1, 1, 16, F16), (64, 3, 5, 8, BF16), (64, 4, 33, 24, F16), (128, 4, 1, 16, BF16), (128, 4, 8, 24, F16), (128, 1, 70, 8, F16),
+    (128, 5, 13, 40, BF16), (256, 2, 1, 16, F16), (256, 3, 11, 32, BF16)])
+def test_attention_over_pages(d, group, nodes, P, dtype):
+    rng = np.random.default_rng(d + 7 * group + nodes)
+    A, H = len(LENGTHS), 2
+    s = Setup(rng, LENGTHS, d, H=H, P=P, L=2, dtype=dtype)
+    Q = rounded(rng.standard_normal((2, A, nodes, H * group, d)), dtype)
+    counts = rng.integers(0, nodes + 1, A).astype(np.int32)
+    counts[::3] = nodes
+    seen = rng.random((A, nodes, nodes)) < 0.5     # any set of drafts, empty ones too: an agent without other tokens sees nothing
+    seen[:, ::4] = False
+    mask = dev(U.pack(seen))
+    kw = dict(counts=dev(counts), mask=mask)
+    for splits in (0, 1, 3):
+        s.check(s.pages.attend_tree(dev(Q, dtype), page_splits=splits, **kw), Q, counts, seen)
+    s.check(s.pages.attend_tree(dev(Q, dtype)), Q, np.full(A, nodes), None)      # neither counts nor mask
+    got = s.pages.attend_tree(dev(Q[1:], dtype), layer_begin=1, layer_end=2, scale=0.2, **kw)
+    s.check(got, Q[1:], counts, seen, layer_begin=1, scale=0.2)
+    pool, dense = _pool(rng, 2, H, d, 75, dtype)
+    for splits, page_splits in ((0, 0), (1, 2), (2, 1)):
+        got = pool.attend_tree(dev(Q, dtype), s.pages, splits=splits, page_splits=page_splits, **kw)
+        s.check(got, Q, counts, seen, pool=dense)
+    got = pool.attend_tree(dev(Q[1:], dtype), s.pages, layer_begin=1, layer_end=2, kernel=_pk().KERNEL_VECTOR, **kw)
+    s.check(got, Q[1:], counts, seen, pool=dense, layer_begin=1)
+
+
+@pytest.mark.parametrize("d,dtype,kw", [(128, F16, dict(value_codec=2)), (256, BF16, dict(value_codec=2)), (64, F16, dict(value_codec=1)),
+                                        (128, BF16, dict(value_codec=5, sign_seed=77)), (128, F16, dict(key_codec=1)), (64, BF16, dict(sign_seed=3))])
+def test_every_kind_of_pool(d, dtype, kw):
+    rng = np.random.default_rng(d)
+    s = Setup(rng, [40, 0, 65], d, L=2, dtype=dtype)
+    pool, dense = _pool(rng, 2, 2, d, 333, dtype, **kw)
+    Q = rounded(rng.standard_normal((2, 3, 4, 6, d)), dtype)
+    seen = U.reach(U.random_trees(rng, 3, 4), [4, 4, 4])
+    for splits in (0, 2):
+        s.check(pool.attend_tree(dev(Q, dtype), s.pages, mask=dev(U.pack(seen)), splits=splits), Q, [4, 4, 4], seen, pool=dense)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_many_rows_and_the_largest_trees(dtype):
+    rng = np.random.default_rng(5)
+    s = Setup(rng, [256, 290, 511], 64, H=1, P=8, dtype=dtype)
+    Q = rounded(rng.standard_normal((1, 3, 256, 3, 64)), dtype)
+    parents = U.random_trees(rng, 3, 256, near=200)
+    counts = np.array([256, 256, 201], np.int32)
+    seen = U.reach(parents, counts)
+    mask, depth = _pk().tree_masks(dev(parents), dev(counts))
+    assert torch.equal(mask.cpu(), torch.from_numpy(U.pack(seen)))
+    s.check(s.pages.attend_tree(dev(Q, dtype), mask=mask, counts=dev(counts)), Q, counts, seen)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_rising_and_far_apart_scores(d, dtype):
+    """Keys that grow along the tokens: a row's reference moves in every tile, by up to hundreds of powers of two, and for some
+    rows the other way round."""
+    rng = np.random.default_rng(d + 1)
+    s = Setup(rng, [700, 333], d, dtype=dtype)
+    for a, n in enumerate(s.lengths):
+        for t in range(n):
+            s.K[:, s.table[a, t // 16], :, t % 16] *= t / 40.0
+    s.K = rounded(s.K, dtype)
+    s.load()
+    Q = rounded(rng.standard_normal((1, 2, 3, 8, d)) * np.array([1.0, -3.0, 0.01])[:, None, None], dtype)
+    for splits in (1, 2):
+        s.check(s.pages.attend_tree(dev(Q, dtype), page_splits=splits), Q, [3, 3], None)
+
+
+def test_queries_and_values_of_extreme_magnitude():
+    rng = np.random.default_rng(11)
+    for dtype, big in ((F16, 6e4), (BF16, 1e30)):
+        s = Setup(rng, [100, 37], 128, dtype=dtype)
+        s.V = rounded(s.V * (big / 8), dtype)
+        s.load()
+        Q = rounded(rng.standard_normal((1, 2, 2, 4, 128)), dtype)
+        s.check(s.pages.attend_tree(dev(Q, dtype)), Q, [2, 2], None)
+        Q[...] = 0.0
+        s.check(s.pages.attend_tree(dev(Q, dtype)), Q, [2, 2], None)
+
+
+@pytest.mark.parametrize("d,dtype", [(64, F16), (128, BF16), (256, F16)])
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+def test_what_a_draft_does_not_see_has_no_effect(d, dtype, bad):
+    """Siblings hold vectors that are not finite: only the drafts that see them are touched."""
+    rng = np.random.default_rng(d)
+    A, N = 3, 12
+    s = Setup(rng, [45, 12, 70], d, dtype=dtype)
+    parents = U.random_trees(rng, A, N, near=4)
+    seen = U.reach(parents, [N] * A)
+    broken = [5, 3, 9]
+    for a, i in enumerate(broken):
+        t = s.lengths[a] - N + i
+        s.K[:, s.table[a, t // 16], :, t % 16] = bad
+        s.V[:, s.table[a, t // 16], :, t % 16, ::3] = bad
+    s.load()
+    Q = rounded(rng.standard_normal((1, A, N, 6, d)), dtype)
+    for a, i in enumerate(broken):      # what the 64-bit form computes for rows that do not see it, without it
+        t = s.lengths[a] - N + i
+        s.K[:, s.table[a, t // 16], :, t % 16] = 0.0
+        s.V[:, s.table[a, t // 16], :, t % 16] = 0.0
+    touched = np.array([seen[a, :, i] for a, i in enumerate(broken)])
+    for splits in (1, 2):
+        got = s.pages.attend_tree(dev(Q, dtype), mask=dev(U.pack(seen)), page_splits=splits)
+        assert not torch.isfinite(got[:, torch.from_numpy(touched)]).any()
+        clean = torch.where(torch.from_numpy(touched).cuda()[None, :, :, None, None], 0.0, got.float())
+        want = Q * ~touched[None, :, :, None, None]
+        s2 = seen & ~touched[:, :, None]
+        out, mag, big = U.attend(want, s.K, s.V, s.table, s.lengths, [N] * A, s2)
+        err = np.abs(clean.double().cpu().numpy() - out)[:, ~touched]
+        tol = U.bound(out, mag, big, d, dtype, 70, 6.0)[:, ~touched]
+        assert (err <= tol).all()
+
+
+def test_pages_that_are_not_there_and_lengths_out_of_range():
+    rng = np.random.default_rng(3)
+    s = Setup(rng, [100, 64, 33], 128, MB=8)
+    s.table[0, 2] = -1
+    s.table[1, 0] = 10_000
+    s.table[1, 3] = -2_000_000_000
+    s.load()
+    Q = rounded(rng.standard_normal((1, 3, 2, 4, 128)), F16)
+    s.check(s.pages.attend_tree(dev(Q, F16)), Q, [2, 2, 2], None)
+    # lengths beyond the table's, negative ones, counts of any size: taken as the nearest bound, entries of -1 are not there
+    s.K, s.V = np.nan_to_num(s.K), np.nan_to_num(s.V)       # (behind its 100 tokens agent 0's last page is no longer empty)
+    s.load()
+    s.pages.lengths.copy_(dev(np.array([2 ** 31 - 1, -5, 33], np.int32)))
+    s.lengths = np.array([128, 0, 33], np.int32)
+    counts = np.array([1000, 1, -7], np.int32)
+    got = s.pages.attend_tree(dev(Q, F16), counts=dev(counts))
+    s.check(got, Q, np.array([2, 0, 0]), None)
+    assert not got[0, 1:].any()
+
+
+def test_chain_equals_dense_tails():
+    """The same step through pool.attend with dense continuations (fp32) and through pages."""
+    pk = _pk()
+    rng = np.random.default_rng(9)
+    lengths, N, d = [20, 3, 70, 129], 3, 128
+    s = Setup(rng, lengths, d, H=2, L=2)
+    pool, _ = _pool(rng, 2, 2, d, 500, F16)
+    Q = dev(rng.standard_normal((2, 4, N, 8, d)), F16)
+    tails = []
+    for a, n in enumerate(lengths):
+        k, v = np.zeros((2, 2, 130, d)), np.zeros((2, 2, 130, d))
+        for t in range(n):
+            k[:, :, t], v[:, :, t] = s.K[:, s.table[a, t // 16], :, t % 16], s.V[:, s.table[a, t // 16], :, t % 16]
+        tails.append((dev(k, F16), dev(v, F16), n))
+    want = pool.attend(Q, tails=tails, tail_causal=True)
+    got = pool.attend_tree(Q, s.pages)
+    # both are within 2e-3 of the exact result, and the second is rounded
+    assert ((got.float() - want).abs() <= 4e-3 + 2.0 ** -11 * want.abs()).all()
+
+
+def test_offsets_beyond_32_bits():
+    """Pages far behind the first 4 GiB of a layer."""
+    pk = _pk()
+    NP, P, H, d = 70_000, 64, 4, 128
+    pages = pk.Pages(1, H, d, NP, 2, 3, page_tokens=P)
+    assert pages.K.numel() * 2 > 2 ** 32 and pages.K.numel() < 2 ** 32
+    rng = np.random.default_rng(1)
+    table = np.array([[NP - 1, 3, NP - 5], [NP - 2, 66_000, 1]], np.int32)
+    lengths = np.array([150, 129], np.int32)
+    K, V = rounded(rng.standard_normal((1, 279, H, d)), F16), rounded(rng.standard_normal((1, 279, H, d)), F16)
+    pages.table.copy_(dev(table))
+    pages.lengths.copy_(dev(lengths))
+    slots = np.concatenate([table[a, np.arange(n) // P] * P + np.arange(n) % P for a, n in enumerate(lengths)]).astype(np.int32)
+    pages.write(dev(K, F16), dev(V, F16), dev(slots))
+    Q = rounded(rng.standard_normal((1, 2, 2, 2 * H, d)), F16)
+    got = pages.attend_tree(dev(Q, F16))
+    small = np.zeros((1, 279, H, 1, d)), np.zeros((1, 279, H, 1, d))      # the same tokens in pages of one
+    small[0][:, :, :, 0], small[1][:, :, :, 0] = K, V
+    where = np.full((2, 150), -1, np.int32)
+    where[0], where[1, :129] = np.arange(150), 150 + np.arange(129)
+    out, mag, big = U.attend(Q, *small, where, lengths, [2, 2], None)
+    err = np.abs(got.double().cpu().numpy() - out)
+    assert (err <= U.bound(out, mag, big, d, F16, 150, 6.0)).all()
+    # an accepted path's vectors move across them
+    parents = np.array([[-1, 0, 0], [-1, 0, 0]], np.int32)
+    tok, fol = np.array([[7, 8, 9], [7, 8, 9]], np.int32), np.array([[9, 0, 5], [8, 1, 0]], np.int32)
+    path, n, after, kept = pages.accept(dev(tok), dev(fol), dev(parents))
+    assert path.tolist() == [[0, 2, -1], [0, 1, -1]] and after.tolist() == [5, 1] and kept.tolist() == [149, 128]
+    assert torch.equal(pages.K[0, NP - 5, :, 148 - 128], dev(K, F16)[0, 149])
+    assert torch.equal(pages.V[0, 66_000, :, 127 - 64], dev(V, F16)[0, 150 + 127])
+
+
+# ------------------------------------------------------------------------------------------------------ tables and slots
+def _state(pages):
+    return [x.cpu().numpy() for x in (pages.table, pages.lengths, pages.free, pages.free_state)]
+
+
+@pytest.mark.parametrize("A,P,MB,NP,n_slots", [(1, 8, 4, 4, 40), (3, 16, 9, 20, 100), (64, 24, 7, 200, 4096), (65, 16, 7, 333, 700),
+                                               (1025, 8, 12, 5000, 40_000), (4096, 8, 5, 9000, 9001)])
+def test_resize_in_many_steps(A, P, MB, NP, n_slots):
+    """Agents grow and shrink at random, sometimes beyond what is free or what the table holds."""
+    pk = _pk()
+    rng = np.random.default_rng(A)
+    pages = pk.Pages(1, 1, 64, NP, A, MB, page_tokens=P)
+    slots = torch.empty(n_slots, dtype=torch.int32, device="cuda")
+    offsets = torch.empty(A + 1, dtype=torch.int32, device="cuda")
+    for step in range(8):
+        table, lengths, ring, state = _state(pages)
+        targets = np.where(rng.random(A) < 0.3, lengths, rng.integers(-2, MB * P + 3, A))
+        if step == 3:
+            targets = np.zeros(A)
+        if step == 5:
+            targets = lengths + rng.integers(0, 3, A)
+        targets = targets.astype(np.int32)
+        want = U.resize(table, lengths, ring, state, targets, P, n_slots)
+        if step % 3 == 2:
+            pages.resize(dev(targets))
+        else:
+            pages.resize(dev(targets), slots, offsets)
+            np.testing.assert_array_equal(slots.cpu().numpy(), want[4])
+            np.testing.assert_array_equal(offsets.cpu().numpy(), want[5])
+        for got, ref in zip(_state(pages), want):
+            np.testing.assert_array_equal(got, ref)
+        # every page is somewhere once
+        t, _, ring, (first, count) = _state(pages)
+        there = np.concatenate([t[t >= 0], ring[(first + np.arange(count)) % NP]])
+        assert sorted(there) == list(range(NP))
+
+
+def test_resize_with_a_broken_state_stays_inside_its_arrays():
+    """Whatever the device arrays hold: table, ring, slots and offsets keep to their bounds (guards on both sides)."""
+    pk = _pk()
+    rng = np.random.default_rng(2)
+    A, MB, NP = 70, 5, 40
+    raw = torch.full((10_000,), 0x5C5C5C5C, dtype=torch.int32, device="cuda")
+    pages = pk.Pages(1, 1, 64, NP, A, MB, page_tokens=8)
+    views, at = [], 1000
+    for n in (A * MB, A, NP, 2, 333, A + 1):
+        views.append(raw[at:at + n])
+        at += n + 500
+    inside = torch.zeros_like(raw, dtype=torch.bool)
+    for v in views:
+        inside[v.storage_offset():v.storage_offset() + v.numel()] = True
+    pages._desc.table_dev, pages._desc.lengths_dev, pages._desc.free_dev, pages._desc.free_state_dev = (v.data_ptr() for v in views[:4])
+    for _ in range(4):
+        for v in views:
+            v.copy_(dev(rng.integers(-2 ** 31, 2 ** 31, v.numel()).astype(np.int32)))
+        views[1].copy_(dev(rng.integers(-10, 60, A).astype(np.int32)))
+        pages.resize(dev(rng.integers(-5, 60, A).astype(np.int32)), views[4], views[5])
+        torch.cuda.synchronize()
+        assert bool((raw[~inside] == 0x5C5C5C5C).all())
+
+
+@pytest.mark.parametrize("d,H,P,dtype,src", [(64, 3, 8, F16, F16), (128, 2, 24, BF16, BF16), (256, 1, 16, F16, torch.float32),
+                                             (128, 8, 16, BF16, torch.float32)])
+def test_write(d, H, P, dtype, src):
+    pk = _pk()
+    rng = np.random.default_rng(d + H)
+    L, NP, n = 3, 11, 37
+    pages = pk.Pages(L, H, d, NP, 1, 1, page_tokens=P, dtype=dtype)
+    pages.K.fill_(7.0)
+    pages.V.fill_(8.0)
+    kv = torch.from_numpy(rng.standard_normal((L, n, 2, H, d)) * 3).to(src).cuda()
+    slots = rng.permutation(NP * P)[:n].astype(np.int32)
+    slots[[0, 5, 9, 36]] = [-1, NP * P, 2 ** 31 - 1, -2 ** 31]
+    wantK, wantV = pages.K.clone(), pages.V.clone()
+    for i, at in enumerate(slots):
+        if 0 <= at < NP * P:
+            wantK[:, at // P, :, at % P], wantV[:, at // P, :, at % P] = kv[:, i, 0].to(dtype), kv[:, i, 1].to(dtype)
+    pages.write(kv[1:, :, 0], kv[1:, :, 1], dev(slots), layer_begin=1)       # side by side, two of three layers
+    assert torch.equal(pages.K[1:], wantK[1:]) and torch.equal(pages.V[1:], wantV[1:])
+    assert bool((pages.K[0] == 7).all()) and bool((pages.V[0] == 8).all())
+    pages.write(kv[:, :, 0].contiguous(), kv[:, :, 1].contiguous(), dev(slots))
+    assert torch.equal(pages.K, wantK) and torch.equal(pages.V, wantV)
+    head_major = kv.permute(0, 3, 2, 1, 4).contiguous().permute(0, 3, 2, 1, 4)      # [layers, heads, 2, tokens, d] in memory
+    pages.K.fill_(7.0)
+    pages.V.fill_(8.0)
+    pages.write(head_major[:, :, 0], head_major[:, :, 1], dev(slots))
+    assert torch.equal(pages.K, wantK) and torch.equal(pages.V, wantV)
+    pages.write(kv[:, :0, 0], kv[:, :0, 1], dev(slots[:0]))                     # nothing
+    one = kv[:, 3:4, 0].expand(L, 2, H, d)                                       # one token for two slots
+    pages.write(one, one, dev(np.array([4, 6], np.int32)))
+    assert torch.equal(pages.K[:, 4 // P, :, 4 % P], kv[:, 3, 0].to(dtype)) and torch.equal(pages.V[:, 6 // P, :, 6 % P], kv[:, 3, 0].to(dtype))
+
+
+# ------------------------------------------------------------------------------------------------------ trees
+@pytest.mark.parametrize("A,N", [(1, 1), (3, 2), (5, 63), (4, 64), (2, 65), (3, 128), (2, 129), (2, 193), (7, 256)])
+@pytest.mark.parametrize("near", [1, 3, 300])
+def test_masks_and_depths(A, N, near):
+    pk = _pk()
+    rng = np.random.default_rng(A + N)
+    parents = U.random_trees(rng, A, N, near)
+    odd = rng.random((A, N)) < 0.1      # further roots, and numbers that are no earlier draft
+    parents[odd] = rng.choice([-1, -9, N, 2 ** 31 - 1, -2 ** 31], odd.sum())
+    parents[0, N // 2] = N // 2
+    counts = rng.integers(-1, N + 2, A).astype(np.int32)
+    for c, used in ((None, np.full(A, N)), (dev(counts), counts)):
+        seen = U.reach(parents, used)
+        mask, depth = pk.tree_masks(dev(parents), c)
+        np.testing.assert_array_equal(mask.cpu().numpy(), U.pack(seen))
+        np.testing.assert_array_equal(depth.cpu().numpy(), np.maximum(seen.sum(-1) - 1, 0))
+
+
+@pytest.mark.parametrize("d,N,P,dtype", [(64, 1, 8, F16), (128, 7, 16, BF16), (64, 64, 24, F16), (256, 40, 8, BF16), (128, 256, 32, F16)])
+def test_accept(d, N, P, dtype):
+    rng = np.random.default_rng(N + d)
+    lengths = [N, N + 1, N + 37, N + 100, max(N - 1, 0), 0, N + 5, N + 64]
+    A = len(lengths)
+    s = Setup(rng, lengths, d, H=3, P=P, L=2, dtype=dtype)
+    parents = U.random_trees(rng, A, N, near=3)
+    parents[1] = np.arange(-1, N - 1)       # a chain, accepted whole
+    tokens = rng.integers(0, 3, (A, N)).astype(np.int32)     # few tokens: children that agree twice, and none
+    following = rng.integers(0, 3, (A, N)).astype(np.int32)
+    tokens[1], following[1] = 5, 5
+    counts = np.array([N, N, N, max(N - 2, 0), N, N, 0, N], np.int32)
+    path, accepted, after, kept = U.accept(tokens, following, parents, counts, s.lengths)
+    Kb, Vb = s.pages.K.clone(), s.pages.V.clone()
+    for c in (dev(counts), None):
+        if c is None:
+            path, accepted, after, kept = U.accept(tokens, following, parents, np.full(A, N), s.lengths)
+        s.pages.K.copy_(Kb)
+        s.pages.V.copy_(Vb)
+        wantK, wantV = Kb.clone(), Vb.clone()
+        for a in range(A):
+            start = kept[a] - accepted[a]
+            for k in range(accepted[a]):
+                src, dst = start + path[a, k], start + k
+                ps, pd = s.table[a, src // P], s.table[a, dst // P]
+                wantK[:, pd, :, dst % P], wantV[:, pd, :, dst % P] = Kb[:, ps, :, src % P], Vb[:, ps, :, src % P]
+        got = s.pages.accept(dev(tokens), dev(following), dev(parents), c)
+        for x, ref in zip(got, (path, accepted, after, kept)):
+            np.testing.assert_array_equal(x.cpu().numpy(), ref)
+        assert torch.equal(s.pages.K.view(torch.int16), wantK.view(torch.int16)) and torch.equal(s.pages.V.view(torch.int16), wantV.view(torch.int16))
+
+
+def test_accept_skips_pages_that_are_not_there():
+    rng = np.random.default_rng(0)
+    s = Setup(rng, [20, 20], 64, P=8, MB=4)
+    s.table[0, 2] = 99
+    s.table[1, 1] = -1
+    s.load()
+    before = s.pages.K.clone()
+    N = 12
+    parents = np.tile(np.where(np.arange(N) < 10, -1, [0] * 10 + [0, 10]), (2, 1)).astype(np.int32)
+    tokens, following = np.full((2, N), 4, np.int32), np.full((2, N), 4, np.int32)
+    path, n, _, _ = s.pages.accept(dev(tokens), dev(following), dev(parents))
+    assert n.tolist() == [3, 3] and path[0, :4].tolist() == [0, 10, 11, -1]
+    # agent 0: both sources lie in the missing page; agent 1: both targets do
+    assert torch.equal(s.pages.K.view(torch.int16), before.view(torch.int16))
+
+
+# ------------------------------------------------------------------------------------------------------ together
+class Step:
+    """A model-less decode step of three agents over a shared pool: room, masks, writes and attention layer by layer, acceptance,
+    and the pages that are not needed go back."""
+
+    def __init__(self, seed, dtype=F16, stream_pool=None):
+        pk = _pk()
+        g = torch.Generator(device="cuda")
+        g.manual_seed(seed)
+        self.L, self.H, self.G, self.d, self.A, self.N = 2, 2, 3, 128, 3, 9
+        r = lambda *s: torch.randn(s, device="cuda", generator=g)  # noqa: E731
+        self.pool = pk.Pool(self.L, self.H, self.d, 400).bind()
+        self.pool.encode(r(self.L, self.H, 400, self.d).to(dtype), r(self.L, self.H, 400, self.d).to(dtype))
+        self.pages = pk.Pages(self.L, self.H, self.d, 40, self.A, 8, page_tokens=8, dtype=dtype)
+        self.pages.K.zero_()
+        self.pages.V.zero_()
+        self.counts = torch.tensor([9, 4, 7], dtype=torch.int32, device="cuda")
+        self.kept = torch.zeros(self.A, dtype=torch.int32, device="cuda")
+        self.target = torch.zeros(self.A, dtype=torch.int32, device="cuda")
+        self.slots = torch.empty(self.A * self.N, dtype=torch.int32, device="cuda")
+        self.offsets = torch.empty(self.A + 1, dtype=torch.int32, device="cuda")
+        self.parents = dev(U.random_trees(np.random.default_rng(seed), self.A, self.N, 3))
+        self.tokens = torch.zeros((self.A, self.N), dtype=torch.int32, device="cuda")
+        self.following = torch.zeros((self.A, self.N), dtype=torch.int32, device="cuda")
+        self.kv = r(self.L, self.A * self.N, 2, self.H, self.d).to(dtype)
+        self.Q = r(self.L, self.A, self.N, self.H * self.G, self.d).to(dtype)
+        self.out = torch.zeros_like(self.Q)
+        self.result = None
+
+    def inputs(self, seed):
+        g = torch.Generator(device="cuda")
+        g.manual_seed(1000 + seed)
+        for x in (self.kv, self.Q):
+            x.copy_(torch.randn(x.shape, device="cuda", generator=g))
+        for x in (self.tokens, self.following):
+            x.copy_(torch.randint(0, 2, x.shape, device="cuda", generator=g))
+
+    def run(self):
+        pk = _pk()
+        torch.add(self.kept, self.counts, out=self.target)
+        self.pages.resize(self.target, self.slots, self.offsets)
+        mask, depth = pk.tree_masks(self.parents, self.counts)
+        for l in range(self.L):
+            self.pages.write(self.kv[l:l + 1, :, 0], self.kv[l:l + 1, :, 1], self.slots, layer_begin=l, layer_end=l + 1)
+            self.pool.attend_tree(self.Q[l:l + 1], self.pages, self.out[l:l + 1], counts=self.counts, mask=mask, layer_begin=l, layer_end=l + 1)
+        self.result = self.pages.accept(self.tokens, self.following, self.parents, self.counts)
+        self.kept.copy_(self.result[3])
+        self.pages.resize(self.kept)
+
+    def state(self):
+        p = self.pages
+        return [x.clone() for x in (self.out, self.kept, self.slots, p.table, p.lengths, p.free, p.free_state, p.K, p.V, *self.result)]
+
+
+def test_a_step_against_the_plain_forms():
+    s = Step(1)
+    p = s.pages
+    Kd, Vd = s.pool.decode(torch.float32)
+    dense = Kd.double().cpu().numpy(), Vd.double().cpu().numpy()
+    for step in range(3):
+        s.inputs(step)
+        was = _state(p)
+        table, lengths, ring, state, slots, _ = U.resize(*was, s.kept.cpu().numpy() + s.counts.cpu().numpy(), 8, 27)
+        K, V = p.K.double().cpu().numpy(), p.V.double().cpu().numpy()
+        kv = s.kv.double().cpu().numpy()
+        for i, at in enumerate(slots):
+            if at >= 0:
+                K[:, at // 8, :, at % 8], V[:, at // 8, :, at % 8] = kv[:, i, 0], kv[:, i, 1]
+        counts = s.counts.cpu().numpy()
+        seen = U.reach(s.parents.cpu().numpy(), counts)
+        Q = s.Q.double().cpu().numpy()
+        out, mag, big = U.attend(Q, K, V, table, lengths, counts, seen, dense)
+        s.run()
+        err = np.abs(s.out.double().cpu().numpy() - out)
+        assert (err <= U.bound(out, mag, big, 128, F16, 500, 6.0, pool=True)).all()
+        want = U.accept(*(x.cpu().numpy() for x in (s.tokens, s.following, s.parents)), counts, lengths)
+        for x, ref in zip(s.result, want):
+            np.testing.assert_array_equal(x.cpu().numpy(), ref)
+        back = U.resize(table, lengths, ring, state, want[3], 8, 0)
+        for got, ref in zip(_state(p), back):
+            np.testing.assert_array_equal(got, ref)
+
+
+def test_captured_steps_follow_the_lengths():
+    """One captured step, replayed: lengths, tables and masks are those of the replay.  Two graphs, captured on one stream and
+    replayed on two, do not disturb each other, and eager steps run in between."""
+    eager, graphed = [Step(1), Step(2)], [Step(1), Step(2)]
+    for s in eager + graphed:
+        s.inputs(0)
+        s.run()
+    torch.cuda.synchronize()
+    graphs = []
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for s in graphed:
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=side):
+                s.run()
+            graphs.append(g)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for step in range(1, 5):
+        for s in eager + graphed:
+            s.inputs(step)
+        torch.cuda.synchronize()
+        for g, st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                g.replay()
+        for s in eager:
+            s.run()
+        torch.cuda.synchronize()
+        for a, b in zip(eager, graphed):
+            for x, y in zip(a.state(), b.state()):
+                assert torch.equal(x, y)
+
+
+def test_on_another_stream_and_twice():
+    """A side stream given by name; the same call again gives the same bits."""
+    rng = np.random.default_rng(4)
+    s = Setup(rng, [300, 10, 64], 128, L=2)
+    pool, _ = _pool(rng, 2, 2, 128, 900, F16)
+    Q = dev(rng.standard_normal((2, 3, 4, 8, 128)), F16)
+    want = pool.attend_tree(Q, s.pages, page_splits=2)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = [pool.attend_tree(Q, s.pages, page_splits=2, stream=side) for _ in range(3)]
+    side.synchronize()
+    assert all(torch.equal(want, x) for x in got)
