@@ -45,16 +45,23 @@ struct TreePlan {
     int layer_begin, layers, nodes, q_heads, G, rows;   // rows = nodes * G of an agent and KV head
     float qscale;
     int nsplit;                // token-range splits of the pages' part
-    int row_tiles;             // 32-row tiles of a wave
+    int waves;                 // row blocks of 32 rows in a workgroup, a wave each: 1, 2 or 4
+    int share;                 // 1 (waves == 1): four waves share the 32 rows
     int row_blocks;            // blocks of rows of an agent and KV head
     FastDiv div_H, div_A, div_G, div_nsplit, div_row_blocks;
     size_t off_ml, off_o, total;   // the pages' partials in the workspace (behind the pool's)
 };
 // Fills in the splits and the row blocks.
 void plan_tree(const PageView& v, int page_splits, TreePlan* t);
-// The pages' part: partials, or, without a pool and splits, the output.
+// The pool's partials, to be joined with the pages': [units][nsplit][agents * rows].
+struct PoolPart {
+    const float *ml, *o;   // nullptr: there is no pool
+    int nsplit, rotated;   // rotated: the value sums are in the rotated domain
+    SignBits signs;
+};
+// The pages' part: partials (out == nullptr), or the output, which takes the pool's partials in.
 hipError_t launch_attend_pages(const PageView& v, const TreePlan& t, bool bf16, const void* Q, float* ml, float* o, void* out,
-                               bool main_kernel, hipStream_t s);
+                               const PoolPart& pool, hipStream_t s);
 // Joins the pool's partials (has_pool) and the pages' and writes the output.
 hipError_t launch_tree_merge(const AttendPlan& plan, const TreePlan& t, bool has_pool, const float* pool_ml, const float* pool_o,
                              const float* ml, const float* o, void* out, hipStream_t s);

@@ -8,6 +8,7 @@
 #include <hip/hip_fp16.h>
 
 #include <mutex>
+#include <type_traits>
 
 #include "polykv_layout.hpp"
 #include "polykv_pages.hpp"
@@ -41,171 +42,385 @@ __device__ __forceinline__ float other_half_sum(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+// Sixteen lanes read 8 bytes each, [4][16] numbers of 16 bits (lanes 4 j .. 4 j + 3: row j), and get a column each.
+__device__ __forceinline__ uint2 lds_transposed(uint16_t* p) {
+    typedef short short4v __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)p));
+}
 // Whether one of the two 16-bit numbers is infinite or NaN.
 template <bool BF> __device__ __forceinline__ bool any_nonfinite(uint32_t w) {
     constexpr uint32_t exponents = BF ? 0x7F807F80u : 0x7C007C00u, one = BF ? 0x00800080u : 0x04000400u;
     return (((w & exponents) + one) & 0x80008000u) != 0;
 }
 
-constexpr int kRaise = 8;   // a row's reference moves when a score is 2^8 times above it
-
-// Tokens [32-token tiles] are the M dimension of the score products and the K dimension of the value products, rows the N
-// dimension of both, so that a lane has one row throughout and its probabilities leave the score accumulators in the order
-// in which they enter the value products (tokens 8 (i / 4) + 4 h + i % 4 of a tile for i < 16, h = lane / 32).
-//   keys    lane (n, h) holds token n's elements 16 j + 8 h .. + 7: a key row's pieces straight from its page, no staging;
-//   values  lane (n, h) loads coordinates (D / 32) n .. of the 16 tokens of its half, whole rows at a time, and makes the products'
-//           operands (eight tokens of one coordinate) of them by byte permutes in registers: value block e of the products
-//           has coordinate (D / 32) m + e in its row m.
-// The tile's page numbers are requested two tiles ahead, its keys when the scores of the tile before are done, its values when
-// that tile's value products are.  Four waves take the tiles of a token range in turn and are joined through LDS at the end.
-template <int D, bool BF, int NT> struct PageTile {
-    static constexpr int KJ = D / 16, VW = D / 64;   // key pieces of a lane; dwords of a value row in a lane
-    tree_uint4 k[KJ];
-    uint32_t v[16][VW];
-};
-
+constexpr int kRows = 32;   // query rows of a wave
 struct TreeArgs {
     PageView v;
     TreePlan t;
     const uint16_t* Q;
-    float *ml, *o;
-    uint16_t* out;   // not nullptr: the rows are complete, written normalized
+    float *ml, *o;   // where partials go
+    uint16_t* out;   // not nullptr: the rows are completed here, with the pool's partials if there are any
+    PoolPart pool;
 };
 
-template <int D, bool BF, int NT>
-__global__ __launch_bounds__(256, NT == 2 && D == 128 ? 1 : D == 256 ? 1 : 2) void attend_pages_kernel(TreeArgs g) {
-    constexpr int ROWS = 32 * NT, MG = D / 32, KJ = D / 16, VW = D / 64, OSTRIDE = D + 4;
-    extern __shared__ __align__(16) float o_s[];   // [4][ROWS][OSTRIDE]
-    __shared__ float m_s[4][ROWS], l_s[4][ROWS];
-    const PageView& v = g.v;
-    const TreePlan& t = g.t;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int h = lane >> 5, n = lane & 31;
+// Both kernels below work on 32-token tiles.  Tokens are the M dimension of the score products and the K dimension of the value
+// products, rows the N dimension of both, so that a lane has one row throughout and its probabilities leave the score
+// accumulators in the order in which they enter the value products (tokens 8 (i / 4) + 4 h + i % 4 of a tile for i < 16, with
+// h = lane / 32, n = lane % 32).
+//   keys    lane (n, h) holds token n's elements 16 j + 8 h .. + 7;
+//   values  lane (n, h) holds coordinates (D / 32) n .. of the 16 tokens of its half and makes the products' operands (eight tokens
+//           of one coordinate) of them by byte permutes: value block e of the products has coordinate (D / 32) m + e in row m.
 
+// Where a workgroup is: which agent, KV head, rows and tiles.
+struct Place {
+    int a, usel, ls, kvh, split, row_block;
+    int length, before, count;   // the agent's tokens, those before its drafts, its drafts
+    bool inside;                 // (the grid is rounded up)
+};
+__device__ __forceinline__ Place place_of(const TreeArgs& g) {
+    const TreePlan& t = g.t;
+    Place p;
     // Workgroup -> (token range of an agent and KV head, row block).  Consecutive workgroups go to the eight dies in turn: the row
     // blocks of a token range follow each other on one die, whose L2 they share.
-    int row_block, split, a, kvh;
     const uint32_t block = blockIdx.y * gridDim.x + blockIdx.x;
-    const int stream = t.div_row_blocks.divide((int)(block >> 3), &row_block) * 8 + (int)(block & 7);
-    if (stream >= t.layers * v.H * v.A * t.nsplit) return;
-    const int ua = t.div_nsplit.divide(stream, &split), usel = t.div_A.divide(ua, &a), ls = t.div_H.divide(usel, &kvh);
-    const int row0 = row_block * ROWS;
+    const int stream = t.div_row_blocks.divide((int)(block >> 3), &p.row_block) * 8 + (int)(block & 7);
+    p.inside = stream < t.layers * g.v.H * g.v.A * t.nsplit;
+    const int ua = t.div_nsplit.divide(stream, &p.split);
+    p.usel = t.div_A.divide(ua, &p.a);
+    p.ls = t.div_H.divide(p.usel, &p.kvh);
+    if (p.inside) {
+        p.length = tokens_of(g.v, p.a);
+        p.count = drafts_of(t.counts, p.a, t.nodes, p.length);
+        p.before = p.length - p.count;
+    }
+    return p;
+}
 
-    const int length = tokens_of(v, a), count = drafts_of(t.counts, a, t.nodes, length), before = length - count;
+// The queries of a wave's rows from row0 on, lane (n, h): row n's elements 16 j + 8 h .. + 7 (rows past the last repeat it), and
+// the draft that the lane's row belongs to.
+template <int D> __device__ __forceinline__ void wait_for(tree_uint4 (&q)[D / 16]) {
+    // Ahead of a loop: otherwise its first product waits for the queries in every round, and with them for all that has been
+    // requested for the rounds to come.
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) asm volatile("" : "+v"(q[j]));
+}
+template <int D> __device__ __forceinline__ int load_queries(const TreeArgs& g, const Place& p, int row0, int lane, tree_uint4 (&q)[D / 16]) {
+    const TreePlan& t = g.t;
+    int in_group;
+    const int draft = t.div_G.divide(min(row0 + (lane & 31), t.rows - 1), &in_group);
+    const uint16_t* src = g.Q + ((((size_t)p.ls * g.v.A + p.a) * t.nodes + draft) * t.q_heads + p.kvh * t.G + in_group) * D + 8 * (lane >> 5);
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) q[j] = *reinterpret_cast<const tree_uint4*>(src + 16 * j);
+    return draft;
+}
+
+// Bit t: draft `draft`'s rows see token t0 + t, among the tile's tokens `there`.
+__device__ __forceinline__ uint32_t seen_tokens(const TreePlan& t, const Place& p, int draft, int t0, uint32_t there) {
+    if (draft >= p.count) return 0;
+    const int lead = t0 - p.before;   // the tile's first token as a draft
+    if (lead + 32 <= 0) return there;
+    uint32_t drafts;
+    if (t.mask == nullptr) {
+        const int n_seen = draft + 1 - lead;   // drafts 0 .. draft
+        drafts = n_seen >= 32 ? 0xFFFFFFFFu : n_seen > 0 ? (1u << n_seen) - 1 : 0u;
+    } else {
+        const uint64_t* row_mask = t.mask + ((size_t)p.a * t.nodes + draft) * t.words;
+        if (lead >= 0) {
+            const int w = lead >> 6, by = lead & 63;
+            drafts = w < t.words ? (uint32_t)(row_mask[w] >> by) : 0u;
+            if (by > 32 && w + 1 < t.words) drafts |= (uint32_t)(row_mask[w + 1] << (64 - by));
+        } else {
+            drafts = (uint32_t)row_mask[0] << -lead;
+        }
+    }
+    if (lead < 0) drafts |= (1u << -lead) - 1;   // the tokens before the drafts
+    return drafts & there;
+}
+
+// A wave's rows: reference (of the scores in base-2 units), sum and value sums, all relative to the reference.  The reference is
+// the maximum of the first tokens that the row sees; it moves when a tile's probabilities sum to more than 2^15 in a lane, a test on
+// a sum that is needed anyway, so most tiles go without maxima.
+template <int D> struct Rows {
+    tree_float16 acc[D / 32];
+    float m, l;
+
+    __device__ __forceinline__ void clear() {
+        m = -INFINITY, l = 0.0f;
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[e][i] = 0.0f;
+    }
+};
+
+// Scores -> probabilities in the pages' type, in operand order.  bfloat16's eight bits leave too much out: a second term holds it.
+template <bool BF> struct Weights {
+    tree_uint4 p[2], low[BF ? 2 : 1];
+};
+template <int D, bool BF> __device__ __forceinline__ Weights<BF> weigh(Rows<D>& r, const tree_float16& s, float qscale) {
+    Weights<BF> w;
+    float sum = 0.0f;
+    bool raise = __ballot(r.m == -INFINITY) != 0;
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {   // (one copy of the code for both passes: two cost the accumulators' registers)
+        if (raise) {
+            float top = s[0];
+            asm volatile("" : "+v"(top));   // (or the maxima are taken for every tile, ahead of the loop)
+#pragma unroll
+            for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+            const float m_new = fmaxf(r.m, other_half_max(top) * qscale);
+            const float f = r.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(r.m - m_new);
+            r.m = m_new;
+            r.l *= f;
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e) r.acc[e] *= f;
+        }
+        const float ref = r.m == -INFINITY ? 0.0f : r.m;   // (a row that has seen nothing yet: weights 0)
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = fmaf(s[i], qscale, -ref);
+        if (__ballot(fabsf(ref) > 65536.0f)) {   // the product's own rounding is more than 2^-8: rounded as it was for the reference
+            float by = qscale;
+            asm volatile("" : "+v"(by));   // (likewise)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = __fsub_rn(__fmul_rn(s[i], by), ref);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(x[i]);
+        sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t two = pack2<BF>(x[2 * i], x[2 * i + 1]);
+            w.p[i >> 2][i & 3] = two;
+            if constexpr (BF) {
+                w.low[i >> 2][i & 3] = pack2<BF>(x[2 * i] - __uint_as_float(two << 16), x[2 * i + 1] - __uint_as_float(two & 0xFFFF0000u));
+                sum += x[2 * i] + x[2 * i + 1];
+            } else {   // (the rounded ones: two at a time)
+                const tree_half2 ones = {(_Float16)1.0f, (_Float16)1.0f};
+                sum = __builtin_amdgcn_fdot2(__builtin_bit_cast(tree_half2, two), ones, sum, false);
+            }
+        }
+        raise = __ballot(sum > 32768.0f) != 0;
+        if (!raise) break;
+    }
+    r.l += sum;
+    return w;
+}
+
+// Value products of 16 tokens: v[x] are the lane's coordinates of the x-th of its eight.
+template <int D, bool BF>
+__device__ __forceinline__ void add_values(Rows<D>& r, const uint32_t (*v)[D / 64], const Weights<BF>& w, int half) {
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) {
+        tree_uint4 a;
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+            a[y] = __builtin_amdgcn_perm(v[2 * y + 1][e >> 1], v[2 * y][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
+        r.acc[e] = tree_mfma<BF>(a, w.p[half], r.acc[e]);
+        if constexpr (BF) r.acc[e] = tree_mfma<BF>(a, w.low[half], r.acc[e]);
+    }
+}
+
+__device__ __forceinline__ size_t out_row(const TreeArgs& g, const Place& p, int r) {
+    int in_group;
+    const int i = g.t.div_G.divide(r, &in_group);
+    return (((size_t)p.ls * g.v.A + p.a) * g.t.nodes + i) * g.t.q_heads + p.kvh * g.t.G + in_group;
+}
+__device__ __forceinline__ size_t partial_row(const TreeArgs& g, const Place& p, int r) {
+    return ((size_t)p.usel * g.t.nsplit + p.split) * ((size_t)g.v.A * g.t.rows) + (size_t)p.a * g.t.rows + r;
+}
+
+// The pool's partials of a row: maximum and sum over its splits.
+__device__ __forceinline__ void pool_sums(const TreeArgs& g, size_t row, size_t stride, float* M, float* L) {
+    *M = -INFINITY, *L = 0.0f;
+    for (int s = 0; s < g.pool.nsplit; ++s) *M = fmaxf(*M, g.pool.ml[(row + s * stride) * 2]);
+    for (int s = 0; s < g.pool.nsplit; ++s) {
+        const float2 part = *reinterpret_cast<const float2*>(g.pool.ml + (row + s * stride) * 2);
+        *L = fmaf(part.y, __builtin_amdgcn_exp2f(part.x - *M), *L);   // (an empty split has m = -inf; the pool is not empty)
+    }
+}
+
+// A wave's rows straight from the registers: partials, or, completed with the pool's, the output.
+// A lane has runs of consecutive coordinates of its row, the two lanes of a row in turn, so the inverse rotation of the pool's part is
+// one exchange with lane ^ 32 and butterflies between registers.
+//   permuted operands    4 runs of 4 MG: run q from MG (8 q + 4 h); accumulator 4 q + j of block e is coordinate MG j + e of it
+//   transposed operands  4 MG runs of 4: run 4 e + q from 32 e + 8 q + 4 h; accumulator 4 q + j of block e is its coordinate j
+template <int D, bool BF, bool TR> __device__ __forceinline__ void store_rows(const TreeArgs& g, const Place& p, const Rows<D>& x, int row0, int lane) {
+    constexpr int MG = D / 32, RUNS = TR ? 4 * MG : 4, C = TR ? 4 : 4 * MG;
+    const int h = lane >> 5, r = row0 + (lane & 31);
+    auto first = [&](int k) { return TR ? 8 * k + 4 * h : C * (2 * k + h); };   // (32 e + 8 q = 8 (4 e + q))
+    auto acc = [&](int k, int c) { return TR ? x.acc[k >> 2][4 * (k & 3) + c] : x.acc[c % MG][4 * k + c / MG]; };
+    float sum = other_half_sum(x.l);
+    const float m = sum == 0.0f ? -INFINITY : x.m;   // the row has seen no token (else its sum is 1 at the least)
+    if (g.out == nullptr) {
+        if (r >= g.t.rows) return;
+        const size_t prow = partial_row(g, p, r);
+        if (sum != 0.0f) {   // (else nobody reads its sums)
+#pragma unroll
+            for (int k = 0; k < RUNS; ++k)
+#pragma unroll
+                for (int c = 0; c < C; c += 4)
+                    *reinterpret_cast<float4*>(g.o + prow * D + first(k) + c) = make_float4(acc(k, c), acc(k, c + 1), acc(k, c + 2), acc(k, c + 3));
+        }
+        if (h == 0) *reinterpret_cast<float2*>(g.ml + prow * 2) = make_float2(m, sum);
+        return;
+    }
+    float y[D / 2];   // [run][coordinate]
+#pragma unroll
+    for (int i = 0; i < D / 2; ++i) y[i] = 0.0f;
+    float weight = 1.0f;
+    if (g.pool.ml != nullptr) {
+        const size_t stride = (size_t)g.v.A * g.t.rows, row = (size_t)p.usel * g.pool.nsplit * stride + (size_t)p.a * g.t.rows + min(r, g.t.rows - 1);
+        float M, L;
+        pool_sums(g, row, stride, &M, &L);
+        const float top = fmaxf(M, m), scale = g.pool.rotated ? (D == 64 ? 0.125f : D == 128 ? 0.08838834764831845f : 0.0625f) : 1.0f;
+        for (int s = 0; s < g.pool.nsplit; ++s) {
+            const float w = __builtin_amdgcn_exp2f(g.pool.ml[(row + s * stride) * 2] - top) * scale;
+            const float* src = g.pool.o + (row + s * stride) * D;
+#pragma unroll
+            for (int k = 0; k < RUNS; ++k)
+#pragma unroll
+                for (int c = 0; c < C; c += 4) {
+                    const float4 z = *reinterpret_cast<const float4*>(src + first(k) + c);
+                    float* d = y + C * k + c;
+                    d[0] = fmaf(z.x, w, d[0]), d[1] = fmaf(z.y, w, d[1]), d[2] = fmaf(z.z, w, d[2]), d[3] = fmaf(z.w, w, d[3]);
+                }
+        }
+        if (g.pool.rotated) {
+            wht_inlane<D / 2>(y);
+#pragma unroll
+            for (int i = 0; i < D / 2; ++i) {
+                const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(y[i]), __float_as_uint(y[i]), false, false);
+                const float low = __uint_as_float(both[0]), high = __uint_as_float(both[1]);
+                y[i] = h ? low - high : low + high;
+            }
+            if (g.pool.signs.on) {
+#pragma unroll
+                for (int k = 0; k < RUNS; ++k)
+                    flip_signs<C>(*reinterpret_cast<float(*)[C]>(y + C * k), sign_word(g.pool.signs, first(k) >> 5) >> (first(k) & 31));
+            }
+        }
+        weight = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);
+        sum = fmaf(sum, weight, L * __builtin_amdgcn_exp2f(M - top));
+    }
+    if (r >= g.t.rows) return;
+    const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+    uint16_t* const dst = g.out + out_row(g, p, r) * D;
+#pragma unroll
+    for (int k = 0; k < RUNS; ++k) {
+        uint32_t z[C / 2];
+#pragma unroll
+        for (int c = 0; c < C; c += 2)
+            z[c / 2] = pack2<BF>(fmaf(acc(k, c), weight, y[C * k + c]) * inv, fmaf(acc(k, c + 1), weight, y[C * k + c + 1]) * inv);
+        if constexpr (TR) {
+            *reinterpret_cast<uint2*>(dst + first(k)) = make_uint2(z[0], z[1]);
+        } else {
+#pragma unroll
+            for (int c = 0; c < C; c += 8)
+                *reinterpret_cast<uint4*>(dst + first(k) + c) = make_uint4(z[c / 2], z[c / 2 + 1], z[c / 2 + 2], z[c / 2 + 3]);
+        }
+    }
+}
+
+// --------------------------------------------------------------------------- up to 32 rows a head ---
+// Keys and values come straight from the pages into registers.  The tile's page numbers are requested two tiles ahead, its keys
+// when the scores of the tile before are done, its values when that tile's value products are.
+// SHARE: the four waves of a workgroup take every fourth tile and are joined through LDS; otherwise a workgroup is one wave.
+constexpr int few_waves_per_simd(int D) { return D == 256 ? 1 : D == 64 ? 3 : 2; }
+
+template <int D, bool BF, bool SHARE>
+__global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D)) void attend_pages_few_kernel(TreeArgs g) {
+    constexpr int MG = D / 32, KJ = D / 16, VW = D / 64, OSTRIDE = D + 4, STEP = SHARE ? 4 : 1;
+    extern __shared__ __align__(16) float o_s[];   // [4][kRows][OSTRIDE] (SHARE)
+    __shared__ float m_s[SHARE ? 4 : 1][kRows], l_s[SHARE ? 4 : 1][kRows];
+    const PageView& v = g.v;
+    const TreePlan& t = g.t;
+    const int tid = threadIdx.x, lane = tid & 63, wave = SHARE ? __builtin_amdgcn_readfirstlane(tid >> 6) : 0;
+    const int h = lane >> 5, n = lane & 31;
+    const Place pl = place_of(g);
+    if (!pl.inside) return;
+    const int row0 = pl.row_block * kRows;
     // the range's tiles; a block of rows that are all behind the agent's drafts sees none
-    const int tiles = row0 < count * t.G ? (length + 31) >> 5 : 0;
-    const int per_split = ((tiles + t.nsplit - 1) / t.nsplit + 3) & ~3;
-    const int t_begin = split * per_split, t_end = min(tiles, t_begin + per_split);
-    const int first = t_begin + wave;
+    const int tiles = row0 < pl.count * t.G ? (pl.length + 31) >> 5 : 0;
+    const int per_split = ((tiles + t.nsplit - 1) / t.nsplit + STEP - 1) & -STEP;
+    const int t_begin = pl.split * per_split, t_end = min(tiles, t_begin + per_split), first = t_begin + wave;
 
-    const size_t layer = (size_t)(t.layer_begin + ls) * v.pages * v.H * v.P * D;
+    const size_t layer = (size_t)(t.layer_begin + pl.ls) * v.pages * v.H * v.P * D;
     const uint16_t* const Kb = v.K + layer;
     const uint16_t* const Vb = v.V + layer;
-    const int32_t* const table = v.table + (size_t)a * v.max_blocks;
-
-    // token of the lane in a tile -> its row among the layer's, -1 if it is not there
+    const int32_t* const table = v.table + (size_t)pl.a * v.max_blocks;
+    // the page of the lane's token in a tile; its row among the layer's, -1 if it is not there
     auto page_at = [&](int tile) {
         int off;
-        const int b = v.div_P.divide(min(32 * tile + n, length - 1), &off);
-        return table[b];
+        return table[v.div_P.divide(min(32 * tile + n, pl.length - 1), &off)];
     };
     auto row_at = [&](int tile, int page) {
         int off;
-        const int tok = 32 * tile + n;
-        (void)v.div_P.divide(tok, &off);
-        return tok < length && (uint32_t)page < (uint32_t)v.pages ? page_row(v, page, kvh, off) : -1;
+        (void)v.div_P.divide(32 * tile + n, &off);
+        return 32 * tile + n < pl.length && (uint32_t)page < (uint32_t)v.pages ? page_row(v, page, pl.kvh, off) : -1;
     };
-    PageTile<D, BF, NT> x;
+    tree_uint4 k[KJ];
+    uint32_t x[16][VW];
     auto load_keys = [&](int row) {
         const uint16_t* src = Kb + (size_t)max(row, 0) * D + 8 * h;
 #pragma unroll
-        for (int j = 0; j < KJ; ++j) x.k[j] = *reinterpret_cast<const tree_uint4*>(src + 16 * j);
+        for (int j = 0; j < KJ; ++j) k[j] = *reinterpret_cast<const tree_uint4*>(src + 16 * j);
     };
     auto load_values = [&](int row) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {   // tokens 8 q + 4 h .. + 3, which lie in one page
-            const int r = __shfl(row, 8 * q + 4 * h, 64);
-            const uint16_t* src = Vb + (size_t)max(r, 0) * D + MG * n;
+            const uint16_t* src = Vb + (size_t)max(__shfl(row, 8 * q + 4 * h, 64), 0) * D + MG * n;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if constexpr (VW == 1) x.v[4 * q + e][0] = *reinterpret_cast<const uint32_t*>(src + e * D);
-                else if constexpr (VW == 2) {
-                    const uint2 w = *reinterpret_cast<const uint2*>(src + e * D);
-                    x.v[4 * q + e][0] = w.x, x.v[4 * q + e][1] = w.y;
-                } else {
-                    const tree_uint4 w = *reinterpret_cast<const tree_uint4*>(src + e * D);
+            for (int e = 0; e < 4; ++e)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x.v[4 * q + e][i] = w[i];
-                }
-            }
+                for (int w = 0; w < VW; ++w) x[4 * q + e][w] = reinterpret_cast<const uint32_t*>(src + e * D)[w];
         }
     };
 
-    tree_float16 acc[NT][MG];
-    float m[NT], l[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        m[nt] = -INFINITY, l[nt] = 0.0f;
-#pragma unroll
-        for (int e = 0; e < MG; ++e)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[nt][e][i] = 0.0f;
-    }
-
+    Rows<D> rows;
+    rows.clear();
     if (first < t_end) {
-        int row = row_at(first, page_at(first));
-        int page = first + 4 < t_end ? page_at(first + 4) : -1;
+        const int first_page = page_at(first);
+        tree_uint4 q[KJ];
+        const int draft = load_queries<D>(g, pl, row0, lane, q);
+        int row = row_at(first, first_page);
         load_keys(row);
         load_values(row);
-        // ---- the block's queries, lane (n, h): row n's elements 16 j + 8 h .. + 7 (rows past the last repeat it)
-        tree_uint4 q[NT][KJ];
-        int draft[NT];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            int in_group;
-            draft[nt] = t.div_G.divide(min(row0 + 32 * nt + n, t.rows - 1), &in_group);
-            const uint16_t* src = g.Q + ((((size_t)ls * v.A + a) * t.nodes + draft[nt]) * t.q_heads + kvh * t.G + in_group) * D + 8 * h;
-#pragma unroll
-            for (int j = 0; j < KJ; ++j) q[nt][j] = *reinterpret_cast<const tree_uint4*>(src + 16 * j);
-        }
-        float poison[NT];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) poison[nt] = 0.0f;
+        int page = first + STEP < t_end ? page_at(first + STEP) : -1;
+        wait_for<D>(q);
+        float poison = 0.0f;
+        if (draft >= pl.count) rows.m = 0.0f;   // such a row never sees a token: any reference will do
 
-        for (int tile = first; tile < t_end; tile += 4) {
-            tree_float16 s[NT];
+        for (int tile = first; tile < t_end; tile += STEP) {
+            tree_float16 s;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
+            for (int i = 0; i < 16; ++i) s[i] = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[nt][i] = 0.0f;
-#pragma unroll
-                for (int j = 0; j < KJ; ++j) s[nt] = tree_mfma<BF>(x.k[j], q[nt][j], s[nt]);
-            }
+            for (int j = 0; j < KJ; ++j) s = tree_mfma<BF>(k[j], q[j], s);
             const int t0 = 32 * tile;
             const uint32_t there = (uint32_t)__ballot(row >= 0);   // (lanes 32 .. 63 repeat the tile's tokens)
-            const bool more = tile + 4 < t_end;
+            const bool more = tile + STEP < t_end;
             int next_row = -1;
             if (more) {
-                next_row = row_at(tile + 4, page);
+                next_row = row_at(tile + STEP, page);
                 load_keys(next_row);
-                page = tile + 8 < t_end ? page_at(tile + 8) : -1;
+                page = tile + 2 * STEP < t_end ? page_at(tile + 2 * STEP) : -1;
             }
-
             // ---- tokens that are not there, and drafts that the lane's draft does not see
-            if (there != 0xFFFFFFFFu || t0 + 32 > before || row0 + ROWS > count * t.G) {
+            if (there != 0xFFFFFFFFu || t0 + 32 > pl.before || row0 + kRows > pl.count * t.G) {
                 uint32_t bad = 0;   // drafts with a value that is not finite
-                if (t0 + 32 > before) {
+                if (t0 + 32 > pl.before) {
 #pragma unroll
                     for (int u = 0; u < 16; ++u) {
                         bool b = false;
 #pragma unroll
-                        for (int w = 0; w < VW; ++w) b |= any_nonfinite<BF>(x.v[u][w]);
+                        for (int w = 0; w < VW; ++w) b |= any_nonfinite<BF>(x[u][w]);
                         const uint64_t lanes = __ballot(b);
                         const int tok = 8 * (u >> 2) + (u & 3);
                         if ((uint32_t)lanes) bad |= 1u << tok;
                         if (lanes >> 32) bad |= 1u << (tok + 4);
                     }
-                    bad &= there & ~(before > t0 ? (1u << (before - t0)) - 1 : 0u);
+                    bad &= there & ~(pl.before > t0 ? (1u << (pl.before - t0)) - 1 : 0u);
                 }
                 const uint32_t kept = there & ~bad;
                 if (kept != 0xFFFFFFFFu) {   // their values are zeroed: a weight of 0 does not undo a NaN
@@ -213,148 +428,251 @@ __global__ __launch_bounds__(256, NT == 2 && D == 128 ? 1 : D == 256 ? 1 : 2) vo
                     for (int u = 0; u < 16; ++u) {
                         const bool keep = (kept >> (8 * (u >> 2) + 4 * h + (u & 3))) & 1;
 #pragma unroll
-                        for (int w = 0; w < VW; ++w) x.v[u][w] = keep ? x.v[u][w] : 0;
+                        for (int w = 0; w < VW; ++w) x[u][w] = keep ? x[u][w] : 0;
                     }
                 }
+                const uint32_t seen = seen_tokens(t, pl, draft, t0, there);
+                if (seen & bad) poison = NAN;
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    uint32_t seen = there;   // bit t: the lane's row sees token t of the tile
-                    const int i = draft[nt];
-                    if (i >= count) seen = 0;
-                    else if (t0 + 32 > before) {
-                        uint32_t drafts = 0;   // bit t: token t is a draft that the row sees
-                        const int lead = t0 - before;   // the tile's first token as a draft
-                        if (t.mask == nullptr) {
-                            const int n_seen = i + 1 - lead;   // drafts 0 .. i
-                            drafts = n_seen >= 32 ? 0xFFFFFFFFu : n_seen > 0 ? (1u << n_seen) - 1 : 0u;
-                        } else {
-                            const uint64_t* row_mask = t.mask + ((size_t)a * t.nodes + i) * t.words;
-                            if (lead >= 0) {
-                                const int w = lead >> 6, by = lead & 63;
-                                drafts = w < t.words ? (uint32_t)(row_mask[w] >> by) : 0u;
-                                if (by > 32 && w + 1 < t.words) drafts |= (uint32_t)(row_mask[w + 1] << (64 - by));
-                            } else {
-                                drafts = (uint32_t)row_mask[0] << -lead;
-                            }
-                        }
-                        if (lead < 0) drafts |= (1u << -lead) - 1;   // the tokens before the drafts
-                        seen &= drafts;
-                    }
-                    if (seen & bad) poison[nt] = NAN;
+                for (int i = 0; i < 16; ++i)
+                    if (!((seen >> (8 * (i >> 2) + 4 * h + (i & 3))) & 1)) s[i] = -INFINITY;
+            }
+            const Weights<BF> w = weigh<D, BF>(rows, s, t.qscale);
+            add_values<D, BF>(rows, x, w, 0);
+            add_values<D, BF>(rows, x + 8, w, 1);
+            if (more) load_values(next_row);
+            row = next_row;
+        }
+        rows.l += poison;
+    }
+    if constexpr (!SHARE) {
+        store_rows<D, BF, false>(g, pl, rows, row0, lane);
+    } else {
+        // ---- the waves' shares
+        const float sum = other_half_sum(rows.l);
+        if (h == 0) m_s[wave][n] = sum == 0.0f ? -INFINITY : rows.m, l_s[wave][n] = sum;   // (no token: sum 0; else 1 at the least)
+        float* dst = o_s + (wave * kRows + n) * OSTRIDE;
 #pragma unroll
-                    for (int k = 0; k < 16; ++k)
-                        if (!((seen >> (8 * (k >> 2) + 4 * h + (k & 3))) & 1)) s[nt][k] = -INFINITY;
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int c = 0; c < MG; ++c) {
+                float y[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[i] = rows.acc[(4 * c + i) % MG][4 * q + (4 * c + i) / MG];
+                *reinterpret_cast<float4*>(dst + MG * (8 * q + 4 * h) + 4 * c) = make_float4(y[0], y[1], y[2], y[3]);
+            }
+        __syncthreads();
+        // eight threads of a row, each with D / 32 groups of four coordinates
+        const int rr = tid >> 3, part = tid & 7, r = row0 + rr;
+        float M = m_s[0][rr];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) M = fmaxf(M, m_s[w][rr]);
+        const float own = M;
+        float L = 0.0f, pool_M = -INFINITY, pool_L = 0.0f;
+        const bool last = g.out != nullptr, with_pool = last && g.pool.ml != nullptr;
+        const size_t stride = (size_t)v.A * t.rows, row = (size_t)pl.usel * g.pool.nsplit * stride + (size_t)pl.a * t.rows + min(r, t.rows - 1);
+        if (with_pool) {
+            pool_sums(g, row, stride, &pool_M, &pool_L);
+            M = fmaxf(M, pool_M);
+        }
+        float f[4];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            f[w] = m_s[w][rr] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_s[w][rr] - M);
+            L += l_s[w][rr] * f[w];
+        }
+        float y[D / 8];
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) y[i] = 0.0f;
+        if (with_pool) {
+            for (int s = 0; s < g.pool.nsplit; ++s) {
+                const float w = __builtin_amdgcn_exp2f(g.pool.ml[(row + s * stride) * 2] - M) *
+                                (g.pool.rotated ? (D == 64 ? 0.125f : D == 128 ? 0.08838834764831845f : 0.0625f) : 1.0f);
+#pragma unroll
+                for (int c = 0; c < MG; ++c) {
+                    const float4 z = *reinterpret_cast<const float4*>(g.pool.o + (row + s * stride) * D + 32 * c + 4 * part);
+                    float* d = y + 4 * c;
+                    d[0] = fmaf(z.x, w, d[0]), d[1] = fmaf(z.y, w, d[1]), d[2] = fmaf(z.z, w, d[2]), d[3] = fmaf(z.w, w, d[3]);
                 }
             }
-
-            // ---- probabilities; the row's reference moves only when a score is far above it
-            tree_uint4 p[NT][2], p_low[NT][2];
+            if (g.pool.rotated) {
+                wht_inlane<D / 8>(y);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                float top = s[nt][0];
-#pragma unroll
-                for (int i = 1; i < 16; ++i) top = fmaxf(top, s[nt][i]);
-                top = other_half_max(top) * t.qscale;
-                if (__ballot(top > m[nt] + kRaise)) {
-                    const float m_new = fmaxf(m[nt], top);
-                    const float f = m[nt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[nt] - m_new);
-                    m[nt] = m_new;
-                    l[nt] *= f;
-#pragma unroll
-                    for (int e = 0; e < MG; ++e) acc[nt][e] *= f;
+                for (int i = 0; i < D / 8; ++i) {
+                    y[i] = wht_lane_stage<1>(y[i], lane);
+                    y[i] = wht_lane_stage<2>(y[i], lane);
+                    y[i] = wht_lane_stage<4>(y[i], lane);
                 }
-                const float ref = m[nt] == -INFINITY ? 0.0f : m[nt];   // (a row that has seen nothing yet: weights 0)
-                float pr[16], sum = 0.0f;
+                if (g.pool.signs.on) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    pr[i] = __builtin_amdgcn_exp2f(fmaf(s[nt][i], t.qscale, -ref));
-                    sum += pr[i];
-                }
-                l[nt] += sum;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t w = pack2<BF>(pr[2 * i], pr[2 * i + 1]);
-                    p[nt][i >> 2][i & 3] = w;
-                    if constexpr (BF)   // what bfloat16's eight bits leave out, as a second term
-                        p_low[nt][i >> 2][i & 3] = pack2<BF>(pr[2 * i] - __uint_as_float(w << 16), pr[2 * i + 1] - __uint_as_float(w & 0xFFFF0000u));
+                    for (int c = 0; c < MG; ++c) flip_signs<4>(*reinterpret_cast<float(*)[4]>(y + 4 * c), sign_word(g.pool.signs, c) >> (4 * part));
                 }
             }
+            L = fmaf(pool_L, __builtin_amdgcn_exp2f(pool_M - M), L);
+        }
+        if (r >= t.rows) return;
+        const float inv = L != 0.0f ? 1.0f / L : 0.0f;
+        const size_t orow = out_row(g, pl, r), prow = partial_row(g, pl, r);
+        const bool any = own != -INFINITY || L != 0.0f;   // (a partial of no tokens: nobody reads its sums)
+#pragma unroll
+        for (int c = 0; c < MG; ++c) {
+            const int at = 32 * c + 4 * part;
+            float* d = y + 4 * c;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float4 z = *reinterpret_cast<const float4*>(o_s + (w * kRows + rr) * OSTRIDE + at);
+                d[0] = fmaf(z.x, f[w], d[0]), d[1] = fmaf(z.y, f[w], d[1]), d[2] = fmaf(z.z, f[w], d[2]), d[3] = fmaf(z.w, f[w], d[3]);
+            }
+            if (last)
+                *reinterpret_cast<uint2*>(g.out + orow * D + at) = make_uint2(pack2<BF>(d[0] * inv, d[1] * inv), pack2<BF>(d[2] * inv, d[3] * inv));
+            else if (any)
+                *reinterpret_cast<float4*>(g.o + prow * D + at) = make_float4(d[0], d[1], d[2], d[3]);
+        }
+        if (!last && part == 0) *reinterpret_cast<float2*>(g.ml + prow * 2) = make_float2(M, L);
+    }
+}
 
-            // ---- values
+// ----------------------------------------------------------------------------- more rows a head ---
+// The waves of a workgroup (two or four) have 32 rows each and walk through the tiles together: a tile is fetched once, whole rows
+// at a time, by all of them, and handed out through LDS, two tiles deep.  A thread fetches pieces of 16 bytes of a few tokens; what it
+// fetches for the tile after the next waits in registers until the tile before is done with.  (Keys straight from the pages as
+// operands, as above, are 32-byte pieces of 32 rows per load: four waves that fetch the same tile that way are bound by the L1.)
+template <int I> using Set = std::integral_constant<int, I>;
+constexpr int many_waves_per_simd(int D) { return D == 256 ? 1 : 2; }
+
+template <int D, bool BF, int W>
+__global__ __launch_bounds__(64 * W, many_waves_per_simd(D)) void attend_pages_many_kernel(TreeArgs g) {
+    constexpr int MG = D / 32, KJ = D / 16;
+    constexpr int LPT = D / 8;                    // threads that fetch a token's row
+    constexpr int TPP = 64 * W / LPT, NP = 32 / TPP;   // tokens of a pass, passes of a tile
+    // Rows in LDS, in halves: 16 bytes more rotate the banks for the keys' operands (16 bytes of each of 32 rows), 64 bytes
+    // more for the values' (32 bytes of each of 4 rows).
+    constexpr int KS = D + 8, VS = D + 32, TILE = 32 * (KS + VS);
+    extern __shared__ __align__(16) uint16_t kv_s[];   // [2 tiles]([32][KS] keys, [32][VS] values)
+    __shared__ int flag_s[2][32];                 // of a tile's token: 1 there, 2 a draft with a value that is not finite
+    const PageView& v = g.v;
+    const TreePlan& t = g.t;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int h = lane >> 5, n = lane & 31;
+    const Place pl = place_of(g);
+    if (!pl.inside) return;
+    const int row0 = pl.row_block * kRows * W;
+    const int tiles = row0 < pl.count * t.G ? (pl.length + 31) >> 5 : 0;
+    const int per_split = (tiles + t.nsplit - 1) / t.nsplit;
+    const int t_begin = pl.split * per_split, t_end = min(tiles, t_begin + per_split);
+    const int my_row0 = row0 + wave * kRows;
+
+    const size_t layer = (size_t)(t.layer_begin + pl.ls) * v.pages * v.H * v.P * D;
+    const uint16_t* const Kb = v.K + layer;
+    const uint16_t* const Vb = v.V + layer;
+    const int32_t* const table = v.table + (size_t)pl.a * v.max_blocks;
+    const int my_token = tid / LPT, piece = tid % LPT;   // of a pass
+    constexpr int SETS = W == 4 ? 2 : 1;
+    int page[NP], page_off[NP];
+    tree_uint4 fk[SETS][NP], fv[SETS][NP];
+    bool fthere[SETS][NP];
+    auto fetch_pages = [&](int tile) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            page[i] = table[v.div_P.divide(min(32 * tile + i * TPP + my_token, pl.length - 1), &page_off[i])];
+        }
+    };
+    auto fetch = [&](int tile, auto set) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            fthere[set][i] = 32 * tile + i * TPP + my_token < pl.length && (uint32_t)page[i] < (uint32_t)v.pages;
+            const size_t at = (size_t)(fthere[set][i] ? page_row(v, page[i], pl.kvh, page_off[i]) : 0) * D + 8 * piece;
+            fk[set][i] = *reinterpret_cast<const tree_uint4*>(Kb + at);
+            fv[set][i] = *reinterpret_cast<const tree_uint4*>(Vb + at);
+        }
+    };
+    auto stage = [&](int tile, auto set) {
+        uint16_t* const dst = kv_s + (tile & 1) * TILE;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int tok = i * TPP + my_token;
+            bool bad = false;
+            if (32 * tile + 32 > pl.before) {
+                const bool mine = any_nonfinite<BF>(fv[set][i][0]) || any_nonfinite<BF>(fv[set][i][1]) || any_nonfinite<BF>(fv[set][i][2]) || any_nonfinite<BF>(fv[set][i][3]);
+                const uint64_t lanes = __ballot(mine);
+                const int group = (lane / LPT) * LPT;   // the lanes that hold the token
+                bad = ((lanes >> group) & (LPT == 64 ? ~0ull : (1ull << LPT) - 1)) != 0 && 32 * tile + tok >= pl.before;
+            }
+            // values that are not there, or not finite, are zeroed: a weight of 0 does not undo a NaN
+            const bool keep = fthere[set][i] && !bad;
+            const tree_uint4 zero = {0, 0, 0, 0};
+            *reinterpret_cast<tree_uint4*>(dst + tok * KS + 8 * piece) = fk[set][i];
+            *reinterpret_cast<tree_uint4*>(dst + 32 * KS + tok * VS + 8 * piece) = keep ? fv[set][i] : zero;
+            if (piece == 0) flag_s[tile & 1][tok] = (fthere[set][i] ? 1 : 0) | (bad && fthere[set][i] ? 2 : 0);
+        }
+    };
+
+    Rows<D> rows;
+    rows.clear();
+    if (t_begin < t_end) {   // (the same for all waves)
+        // Tile t_begin + i waits for LDS in register set i % SETS.
+        auto ask = [&](int tile, auto set) {   // its pages' numbers have been asked for; those of the tile behind it are now
+            if (tile < t_end) fetch(tile, set);
+            if (tile + 1 < t_end) fetch_pages(tile + 1);
+        };
+        fetch_pages(t_begin);
+        ask(t_begin, Set<0>());
+        if constexpr (SETS > 1) ask(t_begin + 1, Set<1 % SETS>());
+        if constexpr (SETS > 2) ask(t_begin + 2, Set<2 % SETS>());
+        tree_uint4 q[KJ];
+        const int draft = load_queries<D>(g, pl, my_row0, lane, q);
+        float poison = 0.0f;
+        if (draft >= pl.count) rows.m = 0.0f;   // such a row never sees a token: any reference will do
+        stage(t_begin, Set<0>());
+        wait_for<D>(q);
+        ask(t_begin + SETS, Set<0>());
+        __syncthreads();
+
+        auto step = [&](int tile, auto next) {   // `next`: the set with the tile behind it
+            uint16_t* const src = kv_s + (tile & 1) * TILE;
+            const int t0 = 32 * tile;
+            tree_float16 s;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < KJ; ++j) s = tree_mfma<BF>(*reinterpret_cast<const tree_uint4*>(src + n * KS + 16 * j + 8 * h), q[j], s);
+            const int flags = flag_s[tile & 1][n];
+            const uint32_t there = (uint32_t)__ballot(flags & 1);
+            if (there != 0xFFFFFFFFu || t0 + 32 > pl.before || my_row0 + kRows > pl.count * t.G) {
+                const uint32_t bad = (uint32_t)__ballot(flags & 2), seen = seen_tokens(t, pl, draft, t0, there);
+                if (seen & bad) poison = NAN;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (!((seen >> (8 * (i >> 2) + 4 * h + (i & 3))) & 1)) s[i] = -INFINITY;
+            }
+            const Weights<BF> w = weigh<D, BF>(rows, s, t.qscale);
+            // values: sixteen lanes read 16 coordinates of four tokens and get four tokens of one coordinate each
+            uint16_t* const vals = src + 32 * KS + (4 * h + ((lane & 15) >> 2)) * VS + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
 #pragma unroll
             for (int half = 0; half < 2; ++half)
 #pragma unroll
                 for (int e = 0; e < MG; ++e) {
-                    tree_uint4 av;
-#pragma unroll
-                    for (int y = 0; y < 4; ++y)
-                        av[y] = __builtin_amdgcn_perm(x.v[8 * half + 2 * y + 1][e >> 1], x.v[8 * half + 2 * y][e >> 1],
-                                                      e & 1 ? 0x07060302u : 0x05040100u);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        acc[nt][e] = tree_mfma<BF>(av, p[nt][half], acc[nt][e]);
-                        if constexpr (BF) acc[nt][e] = tree_mfma<BF>(av, p_low[nt][half], acc[nt][e]);
-                    }
+                    const uint2 lo = lds_transposed(vals + 16 * half * VS + 32 * e), hi = lds_transposed(vals + (16 * half + 8) * VS + 32 * e);
+                    const tree_uint4 a = {lo.x, lo.y, hi.x, hi.y};
+                    rows.acc[e] = tree_mfma<BF>(a, w.p[half], rows.acc[e]);
+                    if constexpr (BF) rows.acc[e] = tree_mfma<BF>(a, w.low[half], rows.acc[e]);
                 }
-            if (more) load_values(next_row);
-            row = next_row;
-        }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) l[nt] += poison[nt];
-    }
-
-    // ---- the waves' shares
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const int r = 32 * nt + n;
-        const float sum = other_half_sum(l[nt]);
-        if (h == 0) m_s[wave][r] = m[nt], l_s[wave][r] = sum;
-        float* dst = o_s + (wave * ROWS + r) * OSTRIDE;
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-            for (int c = 0; c < MG; ++c) {   // coordinates MG (8 q + 4 h) + 4 c ..: accumulator 4 q + j of block e is MG j + e
-                float y[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] = acc[nt][(4 * c + i) % MG][4 * q + (4 * c + i) / MG];
-                *reinterpret_cast<float4*>(dst + MG * (8 * q + 4 * h) + 4 * c) = make_float4(y[0], y[1], y[2], y[3]);
+            if (tile + 1 < t_end) {
+                stage(tile + 1, next);
+                ask(tile + 1 + SETS, next);
             }
-    }
-    __syncthreads();
-
-    constexpr int TPR = 256 / ROWS, CPT = D / (4 * TPR);   // threads of a row, its groups of four coordinates per thread
-    const int rr = tid / TPR, part = tid % TPR, r = row0 + rr;
-    float M = m_s[0][rr];
-#pragma unroll
-    for (int w = 1; w < 4; ++w) M = fmaxf(M, m_s[w][rr]);
-    float f[4], L = 0.0f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        f[w] = m_s[w][rr] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_s[w][rr] - M);
-        L += l_s[w][rr] * f[w];
-    }
-    if (r >= t.rows) return;
-    const bool none = M == -INFINITY && L == 0.0f;   // the row has seen no token
-    const float inv = L != 0.0f ? 1.0f / L : 0.0f;
-    const size_t R = (size_t)v.A * t.rows, prow = ((size_t)usel * t.nsplit + split) * R + (size_t)a * t.rows + r;
-    int in_group;
-    const int i = t.div_G.divide(r, &in_group);
-    const size_t orow = (((size_t)ls * v.A + a) * t.nodes + i) * t.q_heads + kvh * t.G + in_group;
-#pragma unroll
-    for (int c = 0; c < CPT; ++c) {
-        const int at = 4 * (c * TPR + part);
-        float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float4 z = *reinterpret_cast<const float4*>(o_s + (w * ROWS + rr) * OSTRIDE + at);
-            y[0] = fmaf(z.x, f[w], y[0]), y[1] = fmaf(z.y, f[w], y[1]), y[2] = fmaf(z.z, f[w], y[2]), y[3] = fmaf(z.w, f[w], y[3]);
+            __syncthreads();
+        };
+        for (int tile = t_begin; tile < t_end; tile += SETS) {
+            step(tile, Set<1 % SETS>());
+            if constexpr (SETS > 1)
+                if (tile + 1 < t_end) step(tile + 1, Set<2 % SETS>());
+            if constexpr (SETS > 2)
+                if (tile + 2 < t_end) step(tile + 2, Set<0>());
         }
-        if (g.out != nullptr)
-            *reinterpret_cast<uint2*>(g.out + orow * D + at) = make_uint2(pack2<BF>(y[0] * inv, y[1] * inv), pack2<BF>(y[2] * inv, y[3] * inv));
-        else if (!none)
-            *reinterpret_cast<float4*>(g.o + prow * D + at) = make_float4(y[0], y[1], y[2], y[3]);
+        rows.l += poison;
     }
-    if (g.out == nullptr && part == 0) *reinterpret_cast<float2*>(g.ml + prow * 2) = make_float2(M, L);
+    store_rows<D, BF, true>(g, pl, rows, my_row0, lane);
 }
 
 // -------------------------------------------------------------------------------------- merge ---
@@ -423,11 +741,16 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(AttendPlan p, int nspli
 
 // ----------------------------------------------------------------------------------- launchers ---
 void plan_tree(const PageView& v, int page_splits, TreePlan* t) {
-    t->row_tiles = t->rows > 32 && v.D != 256 ? 2 : 1;
-    t->row_blocks = (t->rows + 32 * t->row_tiles - 1) / (32 * t->row_tiles);
+    const int row_tiles = (t->rows + kRows - 1) / kRows;
+    const long tiles = ((long)v.max_blocks * v.P + 31) / 32, units = (long)t->layers * v.H * v.A;
+    t->waves = row_tiles > 2 ? 4 : row_tiles;
+    t->share = units * row_tiles <= 512 ? 1 : 0;
+    if (t->share) t->waves = 1;
+    const int rows = kRows * t->waves;
+    t->row_blocks = (t->rows + rows - 1) / rows;
     // Token ranges: workgroups for 512 places, as far as each of a workgroup's four waves keeps two tiles of the longest
     // continuation there can be.
-    const long groups = (long)t->layers * v.H * v.A * t->row_blocks, tiles = ((long)v.max_blocks * v.P + 31) / 32;
+    const long groups = units * t->row_blocks;
     long want = page_splits > 0 ? page_splits : (512 + groups - 1) / groups;
     const long most = page_splits > 0 ? (tiles + 3) / 4 : tiles / 8;
     if (want > most) want = most;
@@ -446,34 +769,33 @@ static dim3 grid_of(uint64_t workgroups) {
     return workgroups <= most ? dim3((uint32_t)workgroups) : dim3((uint32_t)most, (uint32_t)((workgroups + most - 1) / most));
 }
 
-template <int D, bool BF, int NT>
-static hipError_t launch_pages_one(const TreeArgs& g, dim3 grid, bool main_kernel, hipStream_t s) {
-    constexpr int kShared = 4 * 32 * NT * (D + 4) * (int)sizeof(float);
-    const auto kern = attend_pages_kernel<D, BF, NT>;
-    static std::once_flag configured;
-    static hipError_t config_result = hipSuccess;
-    std::call_once(configured, [&]() {
-        config_result = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kShared);
-    });
-    if (config_result != hipSuccess) return config_result;
-    launch_kernel(kern, grid, dim3(256), kShared, s, main_kernel ? take_kernel_events() : KernelEvents{}, g);
-    return hipGetLastError();
+using PagesKernel = void (*)(TreeArgs);
+struct PagesForm {
+    PagesKernel kern;
+    int threads, shared;
+};
+template <int D, bool BF> static PagesForm pages_form(const TreePlan& t) {
+    constexpr int kShare = 4 * kRows * (D + 4) * (int)sizeof(float), kStage = 2 * 32 * (2 * D + 40) * (int)sizeof(uint16_t);
+    if (t.waves == 4) return {attend_pages_many_kernel<D, BF, 4>, 256, kStage};
+    if (t.waves == 2) return {attend_pages_many_kernel<D, BF, 2>, 128, kStage};
+    if (t.share) return {attend_pages_few_kernel<D, BF, true>, 256, kShare};
+    return {attend_pages_few_kernel<D, BF, false>, 64, 0};
 }
 
 hipError_t launch_attend_pages(const PageView& v, const TreePlan& t, bool bf16, const void* Q, float* ml, float* o, void* out,
-                               bool main_kernel, hipStream_t s) {
-    const TreeArgs g = {v, t, (const uint16_t*)Q, ml, o, (uint16_t*)out};
+                               const PoolPart& pool, hipStream_t s) {
+    const TreeArgs g = {v, t, (const uint16_t*)Q, ml, o, (uint16_t*)out, pool};
     const uint64_t streams = (uint64_t)t.layers * v.H * v.A * t.nsplit;
     const dim3 grid = grid_of((streams + 7) / 8 * 8 * t.row_blocks);
-    if (v.D == 64) {
-        if (t.row_tiles == 2) return bf16 ? launch_pages_one<64, true, 2>(g, grid, main_kernel, s) : launch_pages_one<64, false, 2>(g, grid, main_kernel, s);
-        return bf16 ? launch_pages_one<64, true, 1>(g, grid, main_kernel, s) : launch_pages_one<64, false, 1>(g, grid, main_kernel, s);
+    const PagesForm f = v.D == 64    ? (bf16 ? pages_form<64, true>(t) : pages_form<64, false>(t))
+                        : v.D == 128 ? (bf16 ? pages_form<128, true>(t) : pages_form<128, false>(t))
+                                     : (bf16 ? pages_form<256, true>(t) : pages_form<256, false>(t));
+    if (f.shared > 48 * 1024) {
+        const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(f.kern), hipFuncAttributeMaxDynamicSharedMemorySize, f.shared);
+        if (err != hipSuccess) return err;
     }
-    if (v.D == 128) {
-        if (t.row_tiles == 2) return bf16 ? launch_pages_one<128, true, 2>(g, grid, main_kernel, s) : launch_pages_one<128, false, 2>(g, grid, main_kernel, s);
-        return bf16 ? launch_pages_one<128, true, 1>(g, grid, main_kernel, s) : launch_pages_one<128, false, 1>(g, grid, main_kernel, s);
-    }
-    return bf16 ? launch_pages_one<256, true, 1>(g, grid, main_kernel, s) : launch_pages_one<256, false, 1>(g, grid, main_kernel, s);
+    launch_kernel(f.kern, grid, dim3(f.threads), f.shared, s, take_kernel_events(), g);   // (without a pool: the call's main kernel)
+    return hipGetLastError();
 }
 
 hipError_t launch_tree_merge(const AttendPlan& plan, const TreePlan& t, bool has_pool, const float* pool_ml, const float* pool_o,

@@ -115,7 +115,7 @@ static int make_tree_plan(const polykv_pool* pool, const polykv_pages* pages, co
     }
     size_t off = pool != nullptr ? plan->total : 0;
     t.off_ml = t.off_o = off;
-    if (pool != nullptr || t.nsplit > 1) {
+    if (t.nsplit > 1) {
         off = align_up(off + (size_t)units * t.nsplit * plan->R * 2 * sizeof(float), 256);
         t.off_o = off;
         off = align_up(off + (size_t)units * t.nsplit * plan->R * plan->D * sizeof(float), 256);
@@ -237,18 +237,23 @@ int pool_attend_tree(const polykv_pool* pool, const polykv_pages* pages, const v
     }
     char* ws = reinterpret_cast<char*>(params->workspace_dev);
     const hipStream_t s = (hipStream_t)stream;
-    const bool complete = tree.total == 0;   // nothing to join
     float *ml = reinterpret_cast<float*>(ws + tree.off_ml), *o = reinterpret_cast<float*>(ws + tree.off_o);
-    hipError_t e = launch_attend_pages(page_view(pages), tree, pages->dtype == POLYKV_BF16, Q_dev, ml, o, complete ? out_dev : nullptr,
-                                       pool == nullptr, s);
-    if (e != hipSuccess || complete) return hip_result(e, who);
+    PoolPart part;
+    memset(&part, 0, sizeof(part));
     if (pool != nullptr) {
-        e = launch_attend(pool, plan, Q_dev, nullptr, nullptr, ws, s);
+        const hipError_t e = launch_attend(pool, plan, Q_dev, nullptr, nullptr, ws, s);
         if (e != hipSuccess) return hip_result(e, who);
+        part.ml = reinterpret_cast<const float*>(ws + plan.off_ml);
+        part.o = reinterpret_cast<const float*>(ws + plan.off_o);
+        part.nsplit = plan.nsplit;
+        part.rotated = plan.vcodec != POLYKV_VALUES_INT8;
+        part.signs = plan.signs;
     }
-    return hip_result(launch_tree_merge(plan, tree, pool != nullptr, reinterpret_cast<float*>(ws + plan.off_ml),
-                                        reinterpret_cast<float*>(ws + plan.off_o), ml, o, out_dev, s),
-                      who);
+    // One token range per agent: the pages' kernel completes the rows.  Several: their partials, and the pool's, are joined after it.
+    hipError_t e = launch_attend_pages(page_view(pages), tree, pages->dtype == POLYKV_BF16, Q_dev, ml, o, tree.nsplit == 1 ? out_dev : nullptr,
+                                       part, s);
+    if (e == hipSuccess && tree.nsplit > 1) e = launch_tree_merge(plan, tree, pool != nullptr, part.ml, part.o, ml, o, out_dev, s);
+    return hip_result(e, who);
 }
 
 int polykv_pages_accept(const polykv_pages* pages, const int32_t* tokens_dev, const int32_t* following_dev, const int32_t* parents_dev,

@@ -409,23 +409,9 @@ class Pool:
         return pages._attend_tree(self._h, Q, out, kernel=kernel, splits=splits, key_precision=key_precision, **kw)
 
 
-class _OnDevice:
-    """Calls act on the current device and on streams of it; objects on another one switch to it for the call."""
-
-    def __init__(self, device: torch.device):
-        self.index = device.index if device.index is not None else 0
-        self.guard = None
-
-    def __enter__(self):
-        if torch.cuda.current_device() != self.index:
-            self.guard = torch.cuda.device(self.index)
-            self.guard.__enter__()
-        return self
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            guard, self.guard = self.guard, None
-            guard.__exit__(*exc)
+# Calls act on the current device and on streams of it; an object on another device switches to it for the call.
+def _elsewhere(index: int) -> bool:
+    return (_get_device() if _get_device is not None and torch.cuda.is_initialized() else torch.cuda.current_device()) != index
 
 
 def _new(shape, dtype, device, stream=None):
@@ -450,19 +436,22 @@ def tree_masks(parents: torch.Tensor, counts: torch.Tensor | None = None, mask: 
     nodes], the number of a draft's ancestors -- how far its position is from the first draft's."""
     if parents.dim() != 2 or not parents.is_cuda:
         raise TypeError("parents must be a CUDA tensor [agents, nodes]")
-    agents, nodes = parents.shape
     device = parents.device
+    if _elsewhere(device.index):
+        with torch.cuda.device(device):
+            return tree_masks(parents, counts, mask, depth, stream)
+    shape = parents.shape
+    agents, nodes = shape
     words = (agents, nodes, (nodes + 63) // 64)
-    with _OnDevice(device):
-        if mask is None:
-            mask = _new(words, torch.int64, device, stream)
-        elif mask.dtype is not torch.int64 or mask.shape != words or mask.device != device or not mask.is_contiguous():
-            raise TypeError("mask must be a contiguous int64 tensor of shape %s on %s" % (words, device))
-        if depth is None:
-            depth = _new((agents, nodes), torch.int32, device, stream)
-        _check(lib.polykv_tree_masks(_ints(parents, parents.shape, device, "parents"),
-                                     _ints(counts, (agents,), device, "counts") if counts is not None else None, agents, nodes,
-                                     mask.data_ptr(), _ints(depth, parents.shape, device, "depth"), _stream_ptr(stream)))
+    if mask is None:
+        mask = _new(words, torch.int64, device, stream)
+    elif mask.dtype is not torch.int64 or mask.shape != words or mask.device != device or not mask.is_contiguous():
+        raise TypeError("mask must be a contiguous int64 tensor of shape %s on %s" % (words, device))
+    if depth is None:
+        depth = _new(shape, torch.int32, device, stream)
+    _check(lib.polykv_tree_masks(_ints(parents, shape, device, "parents"),
+                                 _ints(counts, (agents,), device, "counts") if counts is not None else None, agents, nodes,
+                                 mask.data_ptr(), _ints(depth, shape, device, "depth"), _stream_ptr(stream)))
     return mask, depth
 
 
@@ -496,6 +485,8 @@ class Pages:
         self._desc = PagesDesc(layers, kv_heads, head_dim, pages, page_tokens, agents, max_blocks, _DTYPES[dtype],
                                *(t.data_ptr() for t in (self.K, self.V, self.table, self.lengths, self.free, self.free_state)))
         self._ref = C.byref(self._desc)
+        self._index = self.device.index
+        self._per_agent, self._per_offset = self.lengths.shape, torch.Size((agents + 1,))
         self._workspaces = {}   # stream handle -> cached attend_tree workspace
 
     # polykv_pages_resize(targets, slots, offsets)
@@ -504,33 +495,38 @@ class Pages:
         there are no pages, or whose target is out of range, keeps its length.  `slots` (int32, any length) receives the
         places of the tokens that agents grew by, for write(), agent after agent, and -1 behind them; `offsets` (int32
         [agents + 1]) where each agent's begin."""
+        if _elsewhere(self._index):
+            with torch.cuda.device(self._index):
+                return self.resize(targets, slots, offsets, stream)
+        n = 0
         if slots is not None:
             n = slots.numel()
             slots = _ints(slots, (n,), self.device, "slots")
-        else:
-            n = 0
-        with _OnDevice(self.device):
-            _check(lib.polykv_pages_resize(self._ref, _ints(targets, (self.agents,), self.device, "targets"), slots, n,
-                                           _ints(offsets, (self.agents + 1,), self.device, "offsets") if offsets is not None else None,
-                                           _stream_ptr(stream)))
+        if offsets is not None:
+            offsets = _ints(offsets, self._per_offset, self.device, "offsets")
+        _check(lib.polykv_pages_resize(self._ref, _ints(targets, self._per_agent, self.device, "targets"), slots, n, offsets,
+                                       _stream_ptr(stream)))
 
     # polykv_pages_write(K, V, slots)
     def write(self, K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, layer_begin=0, layer_end=None, stream=None):
         """Keys and values [layers of the range, tokens, kv_heads, head_dim] (the pages' dtype or float32; heads' elements
         contiguous, any other strides of whole 16 bytes, the same for both) into the slots of their tokens."""
+        if _elsewhere(self._index):
+            with torch.cuda.device(self._index):
+                return self.write(K, V, slots, layer_begin, layer_end, stream)
         layer_end = self.layers if layer_end is None else layer_end
-        if K.dim() != 4 or K.shape != V.shape or K.shape[0] != layer_end - layer_begin or \
-                K.shape[2] != self.kv_heads or K.shape[3] != self.head_dim:
+        shape, device, dtype = K.shape, self.device, K.dtype
+        if len(shape) != 4 or shape != V.shape or shape[0] != layer_end - layer_begin or shape[2] != self.kv_heads or \
+                shape[3] != self.head_dim:
             raise ValueError("K and V must be [%d, tokens, %d, %d]" % (layer_end - layer_begin, self.kv_heads, self.head_dim))
-        if K.dtype not in (self.dtype, torch.float32) or V.dtype is not K.dtype or K.device != self.device or V.device != self.device:
-            raise TypeError("K and V must be %s or float32 tensors on %s" % (self.dtype, self.device))
+        if (dtype is not self.dtype and dtype is not torch.float32) or V.dtype is not dtype or K.device != device or V.device != device:
+            raise TypeError("K and V must be %s or float32 tensors on %s" % (self.dtype, device))
         strides = K.stride()
         if strides[3] != 1 or V.stride() != strides:
             raise ValueError("K and V must have the same strides, 1 along head_dim")
-        with _OnDevice(self.device):
-            _check(lib.polykv_pages_write(self._ref, K.data_ptr(), V.data_ptr(), _DTYPES[K.dtype], K.shape[1], strides[0], strides[1],
-                                          strides[2], _ints(slots, (K.shape[1],), self.device, "slots"), layer_begin, layer_end,
-                                          _stream_ptr(stream)))
+        _check(lib.polykv_pages_write(self._ref, K.data_ptr(), V.data_ptr(), _DTYPES[dtype], shape[1], strides[0], strides[1],
+                                      strides[2], _ints(slots, (shape[1],), device, "slots"), layer_begin, layer_end,
+                                      _stream_ptr(stream)))
 
     # pool_attend_tree(NULL, Q[drafts], out)
     def attend_tree(self, Q: torch.Tensor, out: torch.Tensor | None = None, **kw):
@@ -544,42 +540,47 @@ class Pages:
     def _attend_tree(self, pool, Q, out, *, counts=None, mask=None, layer_begin=0, layer_end=None, scale=None, kernel=KERNEL_AUTO,
                      splits=0, page_splits=0, key_precision=KEY_PRECISION_EXACT, workspace=None, stream=None):
         device = self.device
+        if _elsewhere(self._index):
+            with torch.cuda.device(device):
+                return self._attend_tree(pool, Q, out, counts=counts, mask=mask, layer_begin=layer_begin, layer_end=layer_end,
+                                         scale=scale, kernel=kernel, splits=splits, page_splits=page_splits,
+                                         key_precision=key_precision, workspace=workspace, stream=stream)
         p = self._tree_params(Q, layer_begin, layer_end, scale, kernel, splits, page_splits, key_precision)
         if Q.device != device:
             raise ValueError("Q is on %s, the pages on %s" % (Q.device, device))
         if counts is not None:
-            p.counts_dev = _ints(counts, (self.agents,), device, "counts")
+            p.counts_dev = _ints(counts, self._per_agent, device, "counts")
         if mask is not None:
             words = (self.agents, p.nodes, (p.nodes + 63) // 64)
             if mask.dtype is not torch.int64 or mask.shape != words or mask.device != device or not mask.is_contiguous():
                 raise TypeError("mask must be a contiguous int64 tensor of shape %s on %s" % (words, device))
             p.mask_dev = mask.data_ptr()
-        with _OnDevice(device):
-            sp = _stream_ptr(stream)
-            ref = C.byref(p)
-            if out is None:
-                out = _new(Q.shape, self.dtype, device, stream)
-            elif out.shape != Q.shape or out.device != device:
-                raise ValueError("out must have Q's shape %s on %s" % (tuple(Q.shape), device))
-            q_ptr, out_ptr = _dev_ptr(Q, self.dtype, "Q"), _dev_ptr(out, self.dtype, "out")
-            # One cached workspace per stream: calls on different streams may overlap and must not share one.  A call that is
-            # being captured gets one of its own from the graph's memory: graphs may be replayed on any streams.
-            capturing = workspace is None and torch.cuda.is_current_stream_capturing()
-            ws = workspace if workspace is not None else None if capturing else self._workspaces.get(sp)
-            if ws is not None:
-                p.workspace_dev, p.workspace_bytes = _dev_ptr(ws, torch.uint8, "workspace"), ws.numel()
-                rc = lib.pool_attend_tree(pool, self._ref, q_ptr, out_ptr, ref, sp)
-                if rc != ENOMEM or workspace is not None:
-                    _check(rc)
-                    return out
-            need = lib.pool_attend_tree_workspace(pool, self._ref, ref)
-            if need:
-                ws = _new((need,), torch.uint8, device, stream)
-                if not capturing:
-                    self._workspaces[sp] = ws
-                p.workspace_dev, p.workspace_bytes = ws.data_ptr(), need
-            _check(lib.pool_attend_tree(pool, self._ref, q_ptr, out_ptr, ref, sp))
-            return out
+        sp = _stream_ptr(stream)
+        ref = C.byref(p)
+        if out is None:
+            out = _new(Q.shape, self.dtype, device, stream)
+        elif out.shape != Q.shape or out.device != device:
+            raise ValueError("out must have Q's shape %s on %s" % (tuple(Q.shape), device))
+        q_ptr, out_ptr = _dev_ptr(Q, self.dtype, "Q"), _dev_ptr(out, self.dtype, "out")
+        # One cached workspace per stream: calls on different streams may overlap and must not share one.  A call that is
+        # being captured gets one of its own from the graph's memory: graphs may be replayed on any streams.
+        own = workspace is None
+        capturing = own and torch.cuda.is_current_stream_capturing()
+        ws = workspace if not own else None if capturing else self._workspaces.get(sp)
+        if ws is not None:
+            p.workspace_dev, p.workspace_bytes = ws.data_ptr() if own else _dev_ptr(ws, torch.uint8, "workspace"), ws.numel()
+            rc = lib.pool_attend_tree(pool, self._ref, q_ptr, out_ptr, ref, sp)
+            if rc != ENOMEM or not own:
+                _check(rc)
+                return out
+        need = lib.pool_attend_tree_workspace(pool, self._ref, ref)
+        if need:
+            ws = _new((need,), torch.uint8, device, stream)
+            if not capturing:
+                self._workspaces[sp] = ws
+            p.workspace_dev, p.workspace_bytes = ws.data_ptr(), need
+        _check(lib.pool_attend_tree(pool, self._ref, q_ptr, out_ptr, ref, sp))
+        return out
 
     def _tree_params(self, Q, layer_begin, layer_end, scale, kernel, splits, page_splits, key_precision):
         layer_end = self.layers if layer_end is None else layer_end
@@ -604,16 +605,20 @@ class Pages:
         the model puts there.  Their keys and values move to right behind the tokens before the drafts, in all layers.
         Returns int32 tensors: path [agents, nodes] (-1 behind the accepted drafts), accepted [agents] (how many), following
         [agents] (the model's token after the last of them) and kept [agents] (the lengths with them, for resize())."""
-        device = self.device
-        if tokens.dim() != 2 or tokens.shape[0] != self.agents:
+        device, shape = self.device, tokens.shape
+        if _elsewhere(self._index):
+            with torch.cuda.device(device):
+                return self.accept(tokens, following, parents, counts, stream)
+        if len(shape) != 2 or shape[0] != self.agents:
             raise ValueError("tokens must be [agents, nodes]")
-        shape = tokens.shape
-        with _OnDevice(device):
+        inputs = (_ints(tokens, shape, device, "tokens"), _ints(following, shape, device, "following"), _ints(parents, shape, device, "parents"),
+                  _ints(counts, self._per_agent, device, "counts") if counts is not None else None)
+        # (one tensor each: they outlive each other)
+        if stream is None:
+            path, accepted, after, kept = torch.empty_like(tokens), *(torch.empty_like(self.lengths) for _ in range(3))
+        else:
             path = _new(shape, torch.int32, device, stream)
-            # (one tensor each: they outlive each other)
-            accepted, after, kept = (_new((self.agents,), torch.int32, device, stream) for _ in range(3))
-            _check(lib.polykv_pages_accept(self._ref, _ints(tokens, shape, device, "tokens"), _ints(following, shape, device, "following"),
-                                           _ints(parents, shape, device, "parents"),
-                                           _ints(counts, (self.agents,), device, "counts") if counts is not None else None, shape[1],
-                                           path.data_ptr(), accepted.data_ptr(), after.data_ptr(), kept.data_ptr(), _stream_ptr(stream)))
+            accepted, after, kept = (_new(self._per_agent, torch.int32, device, stream) for _ in range(3))
+        _check(lib.polykv_pages_accept(self._ref, *inputs, shape[1], path.data_ptr(), accepted.data_ptr(), after.data_ptr(),
+                                       kept.data_ptr(), _stream_ptr(stream)))
         return path, accepted, after, kept

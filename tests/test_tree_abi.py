@@ -130,7 +130,7 @@ def test_attend_refusals_and_sizes():
     assert lib.pool_create(2, 2, 64, 100, C.byref(h)) == pk.OK
     rows = 3 * 4 * 2
     need = lib.pool_attend_tree_workspace(h, d, C.byref(params()))
-    assert need >= 2 * (2 * 2 * rows * (64 + 2) * 4)
+    assert need >= 2 * 2 * rows * (64 + 2) * 4
     assert lib.pool_attend_tree_workspace(None, d, C.byref(params())) == 0          # complete in one launch
     split = lib.pool_attend_tree_workspace(None, d, C.byref(params(page_splits=2)))
     assert split == 0 or split >= 2 * (2 * 2 * rows * (64 + 2) * 4)
