@@ -45,8 +45,9 @@ struct TreePlan {
     int layer_begin, layers, nodes, q_heads, G, rows;   // rows = nodes * G of an agent and KV head
     float qscale;
     int nsplit;                // token-range splits of the pages' part
-    int waves;                 // row blocks of 32 rows in a workgroup, a wave each: 1, 2 or 4
-    int share;                 // 1 (waves == 1): four waves share the 32 rows
+    int wave_rows;             // rows of a wave: 32, or 16 (waves == 1)
+    int waves;                 // waves with rows of their own in a workgroup: 1, 2 or 4
+    int share;                 // 1 (waves == 1): four waves share the rows
     int row_blocks;            // blocks of rows of an agent and KV head
     FastDiv div_H, div_A, div_G, div_nsplit, div_row_blocks;
     size_t off_ml, off_o, total;   // the pages' partials in the workspace (behind the pool's)

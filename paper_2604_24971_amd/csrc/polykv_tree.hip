@@ -20,27 +20,59 @@ typedef _Float16 tree_half2 __attribute__((ext_vector_type(2)));
 typedef __bf16 tree_bf8 __attribute__((ext_vector_type(8)));
 typedef __bf16 tree_bf2 __attribute__((ext_vector_type(2)));
 typedef float tree_float2 __attribute__((ext_vector_type(2)));
+typedef float tree_float4 __attribute__((ext_vector_type(4)));
 typedef float tree_float16 __attribute__((ext_vector_type(16)));
 typedef uint32_t tree_uint4 __attribute__((ext_vector_type(4)));
 
-template <bool BF> __device__ __forceinline__ tree_float16 tree_mfma(const tree_uint4& a, const tree_uint4& b, const tree_float16& c) {
-    if constexpr (BF)
-        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(tree_bf8, a), __builtin_bit_cast(tree_bf8, b), c, 0, 0, 0);
-    else
-        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(tree_half8, a), __builtin_bit_cast(tree_half8, b), c, 0, 0, 0);
+// Products of R x R blocks, R = 32 over 16 elements or 16 over 32.
+template <int R> struct Block;
+template <> struct Block<32> {
+    using Acc = tree_float16;
+};
+template <> struct Block<16> {
+    using Acc = tree_float4;
+};
+template <bool BF, int R>
+__device__ __forceinline__ typename Block<R>::Acc tree_mfma(const tree_uint4& a, const tree_uint4& b, const typename Block<R>::Acc& c) {
+    if constexpr (BF) {
+        const tree_bf8 x = __builtin_bit_cast(tree_bf8, a), y = __builtin_bit_cast(tree_bf8, b);
+        if constexpr (R == 32) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0);
+        else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0);
+    } else {
+        const tree_half8 x = __builtin_bit_cast(tree_half8, a), y = __builtin_bit_cast(tree_half8, b);
+        if constexpr (R == 32) return __builtin_amdgcn_mfma_f32_32x32x16_f16(x, y, c, 0, 0, 0);
+        else return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, c, 0, 0, 0);
+    }
 }
 template <bool BF> __device__ __forceinline__ uint32_t pack2(float x, float y) {   // to nearest even
     const tree_float2 f = {x, y};
     if constexpr (BF) return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, tree_bf2));
     else return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, tree_half2));
 }
-__device__ __forceinline__ float other_half_max(float x) {   // over lanes l and l ^ 32
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+// x of lanes with the bit STEP (32 or 16) clear and set, from every lane of the pair.
+template <int STEP> __device__ __forceinline__ float2 both_lanes(float x) {
+    const uint32_t u = __float_as_uint(x);
+    const auto r = STEP == 32 ? __builtin_amdgcn_permlane32_swap(u, u, false, false) : __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return make_float2(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
-__device__ __forceinline__ float other_half_sum(float x) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+// Over the lanes of a row, lane % R.
+template <int R> __device__ __forceinline__ float row_max(float x) {
+    float2 b = both_lanes<32>(x);
+    x = fmaxf(b.x, b.y);
+    if constexpr (R == 16) {
+        b = both_lanes<16>(x);
+        x = fmaxf(b.x, b.y);
+    }
+    return x;
+}
+template <int R> __device__ __forceinline__ float row_sum(float x) {
+    float2 b = both_lanes<32>(x);
+    x = b.x + b.y;
+    if constexpr (R == 16) {
+        b = both_lanes<16>(x);
+        x = b.x + b.y;
+    }
+    return x;
 }
 // Sixteen lanes read 8 bytes each, [4][16] numbers of 16 bits (lanes 4 j .. 4 j + 3: row j), and get a column each.
 __device__ __forceinline__ uint2 lds_transposed(uint16_t* p) {
@@ -53,7 +85,6 @@ template <bool BF> __device__ __forceinline__ bool any_nonfinite(uint32_t w) {
     return (((w & exponents) + one) & 0x80008000u) != 0;
 }
 
-constexpr int kRows = 32;   // query rows of a wave
 struct TreeArgs {
     PageView v;
     TreePlan t;
@@ -63,13 +94,22 @@ struct TreeArgs {
     PoolPart pool;
 };
 
-// Both kernels below work on 32-token tiles.  Tokens are the M dimension of the score products and the K dimension of the value
-// products, rows the N dimension of both, so that a lane has one row throughout and its probabilities leave the score
-// accumulators in the order in which they enter the value products (tokens 8 (i / 4) + 4 h + i % 4 of a tile for i < 16, with
-// h = lane / 32, n = lane % 32).
-//   keys    lane (n, h) holds token n's elements 16 j + 8 h .. + 7;
-//   values  lane (n, h) holds coordinates (D / 32) n .. of the 16 tokens of its half and makes the products' operands (eight tokens
-//           of one coordinate) of them by byte permutes: value block e of the products has coordinate (D / 32) m + e in row m.
+// Both kernels below work on 32-token tiles, a wave on R = 32 or 16 query rows.  Tokens are the M dimension of the score products
+// and the K dimension of the value products, rows the N dimension of both, so that a lane (n = lane % R, g = lane / R) has row n
+// throughout, and its probabilities leave the score accumulators in the order in which they enter the value products: score i
+// of a lane belongs to token token_of(i).
+//   keys    lane (n, g) holds pieces of 8 elements of tokens n (and, with R = 16, 16 + n);
+//   values  value block e of the products has coordinates of its own in its rows m = 4 LPR q + 4 g + j (accumulator 4 q + j).
+template <int D, int R> struct Shape {
+    static constexpr int LPR = 64 / R;             // lanes of a row
+    static constexpr int KJ = D / (8 * LPR);       // pieces of a token's key in a lane
+    static constexpr int TT = 32 / R;              // score blocks of a tile
+    static constexpr int SN = R / 2;               // scores of a lane
+    static constexpr int PARTS = SN / 8;           // value products over a tile's tokens
+    static constexpr int MG = D / R;               // value blocks
+    static constexpr int AN = R * R / 64;          // accumulators of a block in a lane
+    __device__ static constexpr int token_of(int i) { return 4 * LPR * (i >> 2) + (i & 3); }   // + 4 g
+};
 
 // Where a workgroup is: which agent, KV head, rows and tiles.
 struct Place {
@@ -96,22 +136,22 @@ __device__ __forceinline__ Place place_of(const TreeArgs& g) {
     return p;
 }
 
-// The queries of a wave's rows from row0 on, lane (n, h): row n's elements 16 j + 8 h .. + 7 (rows past the last repeat it), and
-// the draft that the lane's row belongs to.
-template <int D> __device__ __forceinline__ void wait_for(tree_uint4 (&q)[D / 16]) {
-    // Ahead of a loop: otherwise its first product waits for the queries in every round, and with them for all that has been
-    // requested for the rounds to come.
-#pragma unroll
-    for (int j = 0; j < D / 16; ++j) asm volatile("" : "+v"(q[j]));
-}
-template <int D> __device__ __forceinline__ int load_queries(const TreeArgs& g, const Place& p, int row0, int lane, tree_uint4 (&q)[D / 16]) {
+// The queries of a wave's rows from row0 on in operand order (rows past the last repeat it), and the draft of the lane's row.
+template <int D, int R> __device__ __forceinline__ int load_queries(const TreeArgs& g, const Place& p, int row0, int lane, tree_uint4 (&q)[Shape<D, R>::KJ]) {
     const TreePlan& t = g.t;
+    constexpr int LPR = 64 / R;
     int in_group;
-    const int draft = t.div_G.divide(min(row0 + (lane & 31), t.rows - 1), &in_group);
-    const uint16_t* src = g.Q + ((((size_t)p.ls * g.v.A + p.a) * t.nodes + draft) * t.q_heads + p.kvh * t.G + in_group) * D + 8 * (lane >> 5);
+    const int draft = t.div_G.divide(min(row0 + lane % R, t.rows - 1), &in_group);
+    const uint16_t* src = g.Q + ((((size_t)p.ls * g.v.A + p.a) * t.nodes + draft) * t.q_heads + p.kvh * t.G + in_group) * D + 8 * (lane / R);
 #pragma unroll
-    for (int j = 0; j < D / 16; ++j) q[j] = *reinterpret_cast<const tree_uint4*>(src + 16 * j);
+    for (int j = 0; j < Shape<D, R>::KJ; ++j) q[j] = *reinterpret_cast<const tree_uint4*>(src + 8 * LPR * j);
     return draft;
+}
+// Ahead of a loop: otherwise its first product waits for the queries in every round, and with them for all that has been requested
+// for the rounds to come.
+template <int N> __device__ __forceinline__ void wait_for(tree_uint4 (&q)[N]) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) asm volatile("" : "+v"(q[j]));
 }
 
 // Bit t: draft `draft`'s rows see token t0 + t, among the tile's tokens `there`.
@@ -137,59 +177,83 @@ __device__ __forceinline__ uint32_t seen_tokens(const TreePlan& t, const Place& 
     return drafts & there;
 }
 
+// The scores of a lane.
+template <int R> struct Scores {
+    typename Block<R>::Acc t[32 / R];
+
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int u = 0; u < 32 / R; ++u)
+#pragma unroll
+            for (int i = 0; i < R * R / 64; ++i) t[u][i] = 0.0f;
+    }
+    __device__ __forceinline__ float get(int i) const { return R == 32 ? t[0][i] : t[i >> 2 & (32 / R - 1)][i & 3]; }
+    __device__ __forceinline__ void set(int i, float x) {
+        if constexpr (R == 32) t[0][i] = x;
+        else t[i >> 2][i & 3] = x;
+    }
+};
+template <int D, int R> __device__ __forceinline__ void hide_unseen(Scores<R>& s, uint32_t seen, int g) {
+    seen >>= 4 * g;
+#pragma unroll
+    for (int i = 0; i < Shape<D, R>::SN; ++i)
+        if (!((seen >> Shape<D, R>::token_of(i)) & 1)) s.set(i, -INFINITY);
+}
+
 // A wave's rows: reference (of the scores in base-2 units), sum and value sums, all relative to the reference.  The reference is
 // the maximum of the first tokens that the row sees; it moves when a tile's probabilities sum to more than 2^15 in a lane, a test on
 // a sum that is needed anyway, so most tiles go without maxima.
-template <int D> struct Rows {
-    tree_float16 acc[D / 32];
+template <int D, int R> struct Rows {
+    typename Block<R>::Acc acc[D / R];
     float m, l;
 
     __device__ __forceinline__ void clear() {
         m = -INFINITY, l = 0.0f;
 #pragma unroll
-        for (int e = 0; e < D / 32; ++e)
+        for (int e = 0; e < D / R; ++e)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[e][i] = 0.0f;
+            for (int i = 0; i < R * R / 64; ++i) acc[e][i] = 0.0f;
     }
 };
 
 // Scores -> probabilities in the pages' type, in operand order.  bfloat16's eight bits leave too much out: a second term holds it.
-template <bool BF> struct Weights {
-    tree_uint4 p[2], low[BF ? 2 : 1];
+template <bool BF, int R> struct Weights {
+    tree_uint4 p[R / 16], low[BF ? R / 16 : 1];
 };
-template <int D, bool BF> __device__ __forceinline__ Weights<BF> weigh(Rows<D>& r, const tree_float16& s, float qscale) {
-    Weights<BF> w;
+template <int D, bool BF, int R> __device__ __forceinline__ Weights<BF, R> weigh(Rows<D, R>& r, const Scores<R>& s, float qscale) {
+    constexpr int SN = Shape<D, R>::SN;
+    Weights<BF, R> w;
     float sum = 0.0f;
     bool raise = __ballot(r.m == -INFINITY) != 0;
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {   // (one copy of the code for both passes: two cost the accumulators' registers)
         if (raise) {
-            float top = s[0];
+            float top = s.get(0);
             asm volatile("" : "+v"(top));   // (or the maxima are taken for every tile, ahead of the loop)
 #pragma unroll
-            for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-            const float m_new = fmaxf(r.m, other_half_max(top) * qscale);
+            for (int i = 1; i < SN; ++i) top = fmaxf(top, s.get(i));
+            const float m_new = fmaxf(r.m, row_max<R>(top) * qscale);
             const float f = r.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(r.m - m_new);
             r.m = m_new;
             r.l *= f;
 #pragma unroll
-            for (int e = 0; e < D / 32; ++e) r.acc[e] *= f;
+            for (int e = 0; e < D / R; ++e) r.acc[e] *= f;
         }
         const float ref = r.m == -INFINITY ? 0.0f : r.m;   // (a row that has seen nothing yet: weights 0)
-        float x[16];
+        float x[SN];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = fmaf(s[i], qscale, -ref);
+        for (int i = 0; i < SN; ++i) x[i] = fmaf(s.get(i), qscale, -ref);
         if (__ballot(fabsf(ref) > 65536.0f)) {   // the product's own rounding is more than 2^-8: rounded as it was for the reference
             float by = qscale;
             asm volatile("" : "+v"(by));   // (likewise)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = __fsub_rn(__fmul_rn(s[i], by), ref);
+            for (int i = 0; i < SN; ++i) x[i] = __fsub_rn(__fmul_rn(s.get(i), by), ref);
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(x[i]);
+        for (int i = 0; i < SN; ++i) x[i] = __builtin_amdgcn_exp2f(x[i]);
         sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < SN / 2; ++i) {
             const uint32_t two = pack2<BF>(x[2 * i], x[2 * i + 1]);
             w.p[i >> 2][i & 3] = two;
             if constexpr (BF) {
@@ -207,20 +271,7 @@ template <int D, bool BF> __device__ __forceinline__ Weights<BF> weigh(Rows<D>& 
     return w;
 }
 
-// Value products of 16 tokens: v[x] are the lane's coordinates of the x-th of its eight.
-template <int D, bool BF>
-__device__ __forceinline__ void add_values(Rows<D>& r, const uint32_t (*v)[D / 64], const Weights<BF>& w, int half) {
-#pragma unroll
-    for (int e = 0; e < D / 32; ++e) {
-        tree_uint4 a;
-#pragma unroll
-        for (int y = 0; y < 4; ++y)
-            a[y] = __builtin_amdgcn_perm(v[2 * y + 1][e >> 1], v[2 * y][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
-        r.acc[e] = tree_mfma<BF>(a, w.p[half], r.acc[e]);
-        if constexpr (BF) r.acc[e] = tree_mfma<BF>(a, w.low[half], r.acc[e]);
-    }
-}
-
+// Row r of the agent in Q and out, and among the partials.
 __device__ __forceinline__ size_t out_row(const TreeArgs& g, const Place& p, int r) {
     int in_group;
     const int i = g.t.div_G.divide(r, &in_group);
@@ -229,6 +280,8 @@ __device__ __forceinline__ size_t out_row(const TreeArgs& g, const Place& p, int
 __device__ __forceinline__ size_t partial_row(const TreeArgs& g, const Place& p, int r) {
     return ((size_t)p.usel * g.t.nsplit + p.split) * ((size_t)g.v.A * g.t.rows) + (size_t)p.a * g.t.rows + r;
 }
+
+constexpr float kRotation(int D) { return D == 64 ? 0.125f : D == 128 ? 0.08838834764831845f : 0.0625f; }
 
 // The pool's partials of a row: maximum and sum over its splits.
 __device__ __forceinline__ void pool_sums(const TreeArgs& g, size_t row, size_t stride, float* M, float* L) {
@@ -241,16 +294,17 @@ __device__ __forceinline__ void pool_sums(const TreeArgs& g, size_t row, size_t 
 }
 
 // A wave's rows straight from the registers: partials, or, completed with the pool's, the output.
-// A lane has runs of consecutive coordinates of its row, the two lanes of a row in turn, so the inverse rotation of the pool's part is
-// one exchange with lane ^ 32 and butterflies between registers.
-//   permuted operands    4 runs of 4 MG: run q from MG (8 q + 4 h); accumulator 4 q + j of block e is coordinate MG j + e of it
-//   transposed operands  4 MG runs of 4: run 4 e + q from 32 e + 8 q + 4 h; accumulator 4 q + j of block e is its coordinate j
-template <int D, bool BF, bool TR> __device__ __forceinline__ void store_rows(const TreeArgs& g, const Place& p, const Rows<D>& x, int row0, int lane) {
-    constexpr int MG = D / 32, RUNS = TR ? 4 * MG : 4, C = TR ? 4 : 4 * MG;
-    const int h = lane >> 5, r = row0 + (lane & 31);
-    auto first = [&](int k) { return TR ? 8 * k + 4 * h : C * (2 * k + h); };   // (32 e + 8 q = 8 (4 e + q))
-    auto acc = [&](int k, int c) { return TR ? x.acc[k >> 2][4 * (k & 3) + c] : x.acc[c % MG][4 * k + c / MG]; };
-    float sum = other_half_sum(x.l);
+// A lane has runs of consecutive coordinates of its row, the row's lanes in turn, so the inverse rotation of the pool's part is an
+// exchange with each of the row's other lanes and butterflies between registers.
+//   permuted operands    block e has coordinates MG m + e: R / (4 LPR) runs of 4 MG, run k from MG (4 LPR k + 4 g)
+//   transposed operands  block e has coordinates R e + m: D / (4 LPR) runs of 4, run k from 4 LPR k + 4 g
+template <int D, bool BF, int R, bool TR>
+__device__ __forceinline__ void store_rows(const TreeArgs& g, const Place& p, const Rows<D, R>& x, int row0, int lane) {
+    constexpr int MG = D / R, LPR = 64 / R, C = TR ? 4 : 4 * MG, RUNS = D / (LPR * C), PER = R / (4 * LPR);   // PER: runs of a block
+    const int h = lane / R, r = row0 + lane % R;
+    auto first = [&](int k) { return C * (LPR * k + h); };
+    auto acc = [&](int k, int c) { return TR ? x.acc[k / PER][4 * (k % PER) + c] : x.acc[c % MG][4 * k + c / MG]; };
+    float sum = row_sum<R>(x.l);
     const float m = sum == 0.0f ? -INFINITY : x.m;   // the row has seen no token (else its sum is 1 at the least)
     if (g.out == nullptr) {
         if (r >= g.t.rows) return;
@@ -265,15 +319,16 @@ template <int D, bool BF, bool TR> __device__ __forceinline__ void store_rows(co
         if (h == 0) *reinterpret_cast<float2*>(g.ml + prow * 2) = make_float2(m, sum);
         return;
     }
-    float y[D / 2];   // [run][coordinate]
+    constexpr int N = D / LPR;   // coordinates of a lane
+    float y[N];
 #pragma unroll
-    for (int i = 0; i < D / 2; ++i) y[i] = 0.0f;
+    for (int i = 0; i < N; ++i) y[i] = 0.0f;
     float weight = 1.0f;
     if (g.pool.ml != nullptr) {
         const size_t stride = (size_t)g.v.A * g.t.rows, row = (size_t)p.usel * g.pool.nsplit * stride + (size_t)p.a * g.t.rows + min(r, g.t.rows - 1);
         float M, L;
         pool_sums(g, row, stride, &M, &L);
-        const float top = fmaxf(M, m), scale = g.pool.rotated ? (D == 64 ? 0.125f : D == 128 ? 0.08838834764831845f : 0.0625f) : 1.0f;
+        const float top = fmaxf(M, m), scale = g.pool.rotated ? kRotation(D) : 1.0f;
         for (int s = 0; s < g.pool.nsplit; ++s) {
             const float w = __builtin_amdgcn_exp2f(g.pool.ml[(row + s * stride) * 2] - top) * scale;
             const float* src = g.pool.o + (row + s * stride) * D;
@@ -287,17 +342,23 @@ template <int D, bool BF, bool TR> __device__ __forceinline__ void store_rows(co
                 }
         }
         if (g.pool.rotated) {
-            wht_inlane<D / 2>(y);
+            wht_inlane<N>(y);
 #pragma unroll
-            for (int i = 0; i < D / 2; ++i) {
-                const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(y[i]), __float_as_uint(y[i]), false, false);
-                const float low = __uint_as_float(both[0]), high = __uint_as_float(both[1]);
-                y[i] = h ? low - high : low + high;
+            for (int i = 0; i < N; ++i) {
+                float2 b = both_lanes<32>(y[i]);
+                y[i] = lane & 32 ? b.x - b.y : b.x + b.y;
+                if constexpr (R == 16) {
+                    b = both_lanes<16>(y[i]);
+                    y[i] = lane & 16 ? b.x - b.y : b.x + b.y;
+                }
             }
             if (g.pool.signs.on) {
+                constexpr int W = C < 32 ? C : 32;   // coordinates of one word of signs
 #pragma unroll
                 for (int k = 0; k < RUNS; ++k)
-                    flip_signs<C>(*reinterpret_cast<float(*)[C]>(y + C * k), sign_word(g.pool.signs, first(k) >> 5) >> (first(k) & 31));
+#pragma unroll
+                    for (int c = 0; c < C; c += W)
+                        flip_signs<W>(*reinterpret_cast<float(*)[W]>(y + C * k + c), sign_word(g.pool.signs, (first(k) + c) >> 5) >> ((first(k) + c) & 31));
             }
         }
         weight = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);
@@ -322,24 +383,26 @@ template <int D, bool BF, bool TR> __device__ __forceinline__ void store_rows(co
     }
 }
 
-// --------------------------------------------------------------------------- up to 32 rows a head ---
-// Keys and values come straight from the pages into registers.  The tile's page numbers are requested two tiles ahead, its keys
-// when the scores of the tile before are done, its values when that tile's value products are.
+// ---------------------------------------------------------------------------- few rows a head ---
+// A wave's keys and values come straight from the pages into registers.  The tile's page numbers are requested two tiles ahead, its
+// keys when the scores of the tile before are done, its values when that tile's value products are.  A lane loads MG coordinates
+// of the tokens that its scores belong to and makes operands (eight tokens of one coordinate) of them by byte permutes.
 // SHARE: the four waves of a workgroup take every fourth tile and are joined through LDS; otherwise a workgroup is one wave.
-constexpr int few_waves_per_simd(int D) { return D == 256 ? 1 : D == 64 ? 3 : 2; }
+constexpr int few_waves_per_simd(int D, int R) { return R == 16 ? (D == 64 ? 4 : D == 128 ? 3 : 2) : D == 64 ? 3 : 2; }
 
-template <int D, bool BF, bool SHARE>
-__global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D)) void attend_pages_few_kernel(TreeArgs g) {
-    constexpr int MG = D / 32, KJ = D / 16, VW = D / 64, OSTRIDE = D + 4, STEP = SHARE ? 4 : 1;
-    extern __shared__ __align__(16) float o_s[];   // [4][kRows][OSTRIDE] (SHARE)
-    __shared__ float m_s[SHARE ? 4 : 1][kRows], l_s[SHARE ? 4 : 1][kRows];
+template <int D, bool BF, int R, bool SHARE>
+__global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D, R)) void attend_pages_few_kernel(TreeArgs g) {
+    using S = Shape<D, R>;
+    constexpr int MG = S::MG, KJ = S::KJ, SN = S::SN, VW = MG / 2, OSTRIDE = D + 4, STEP = SHARE ? 4 : 1;
+    extern __shared__ __align__(16) float o_s[];   // [4][R][OSTRIDE] (SHARE)
+    __shared__ float m_s[SHARE ? 4 : 1][R], l_s[SHARE ? 4 : 1][R];
     const PageView& v = g.v;
     const TreePlan& t = g.t;
     const int tid = threadIdx.x, lane = tid & 63, wave = SHARE ? __builtin_amdgcn_readfirstlane(tid >> 6) : 0;
-    const int h = lane >> 5, n = lane & 31;
+    const int h = lane / R, n = lane % R;
     const Place pl = place_of(g);
     if (!pl.inside) return;
-    const int row0 = pl.row_block * kRows;
+    const int row0 = pl.row_block * R;
     // the range's tiles; a block of rows that are all behind the agent's drafts sees none
     const int tiles = row0 < pl.count * t.G ? (pl.length + 31) >> 5 : 0;
     const int per_split = ((tiles + t.nsplit - 1) / t.nsplit + STEP - 1) & -STEP;
@@ -349,54 +412,72 @@ __global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D)) void atten
     const uint16_t* const Kb = v.K + layer;
     const uint16_t* const Vb = v.V + layer;
     const int32_t* const table = v.table + (size_t)pl.a * v.max_blocks;
-    // the page of the lane's token in a tile; its row among the layer's, -1 if it is not there
+    // lane l looks after token l % 32 of a tile: its page; its row among the layer's, -1 if it is not there
     auto page_at = [&](int tile) {
         int off;
-        return table[v.div_P.divide(min(32 * tile + n, pl.length - 1), &off)];
+        return table[v.div_P.divide(min(32 * tile + (lane & 31), pl.length - 1), &off)];
     };
     auto row_at = [&](int tile, int page) {
         int off;
-        (void)v.div_P.divide(32 * tile + n, &off);
-        return 32 * tile + n < pl.length && (uint32_t)page < (uint32_t)v.pages ? page_row(v, page, pl.kvh, off) : -1;
+        const int tok = 32 * tile + (lane & 31);
+        (void)v.div_P.divide(tok, &off);
+        return tok < pl.length && (uint32_t)page < (uint32_t)v.pages ? page_row(v, page, pl.kvh, off) : -1;
     };
-    tree_uint4 k[KJ];
-    uint32_t x[16][VW];
+    tree_uint4 k[S::TT][KJ];
+    uint32_t x[SN][VW];
     auto load_keys = [&](int row) {
-        const uint16_t* src = Kb + (size_t)max(row, 0) * D + 8 * h;
 #pragma unroll
-        for (int j = 0; j < KJ; ++j) k[j] = *reinterpret_cast<const tree_uint4*>(src + 16 * j);
+        for (int u = 0; u < S::TT; ++u) {
+            const int r = R == 32 ? row : __shfl(row, 16 * u + n, 64);
+            const uint16_t* src = Kb + (size_t)max(r, 0) * D + 8 * h;
+#pragma unroll
+            for (int j = 0; j < KJ; ++j) k[u][j] = *reinterpret_cast<const tree_uint4*>(src + 8 * S::LPR * j);
+        }
     };
     auto load_values = [&](int row) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {   // tokens 8 q + 4 h .. + 3, which lie in one page
-            const uint16_t* src = Vb + (size_t)max(__shfl(row, 8 * q + 4 * h, 64), 0) * D + MG * n;
+        for (int q = 0; q < SN / 4; ++q) {   // four tokens at a time, which lie in one page
+            const uint16_t* src = Vb + (size_t)max(__shfl(row, S::token_of(4 * q) + 4 * h, 64), 0) * D + MG * n;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t* at = reinterpret_cast<const uint32_t*>(src + e * D);
+                if constexpr (VW == 1) {
+                    x[4 * q + e][0] = at[0];
+                } else if constexpr (VW == 2) {
+                    const uint2 w = *reinterpret_cast<const uint2*>(at);
+                    x[4 * q + e][0] = w.x, x[4 * q + e][1] = w.y;
+                } else {
 #pragma unroll
-                for (int w = 0; w < VW; ++w) x[4 * q + e][w] = reinterpret_cast<const uint32_t*>(src + e * D)[w];
+                    for (int c = 0; c < VW; c += 4) {
+                        const tree_uint4 w = *reinterpret_cast<const tree_uint4*>(at + c);
+                        x[4 * q + e][c] = w[0], x[4 * q + e][c + 1] = w[1], x[4 * q + e][c + 2] = w[2], x[4 * q + e][c + 3] = w[3];
+                    }
+                }
+            }
         }
     };
 
-    Rows<D> rows;
+    Rows<D, R> rows;
     rows.clear();
     if (first < t_end) {
         const int first_page = page_at(first);
         tree_uint4 q[KJ];
-        const int draft = load_queries<D>(g, pl, row0, lane, q);
+        const int draft = load_queries<D, R>(g, pl, row0, lane, q);
         int row = row_at(first, first_page);
         load_keys(row);
         load_values(row);
         int page = first + STEP < t_end ? page_at(first + STEP) : -1;
-        wait_for<D>(q);
+        wait_for(q);
         float poison = 0.0f;
         if (draft >= pl.count) rows.m = 0.0f;   // such a row never sees a token: any reference will do
 
         for (int tile = first; tile < t_end; tile += STEP) {
-            tree_float16 s;
+            Scores<R> s;
+            s.clear();
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+            for (int j = 0; j < KJ; ++j)
 #pragma unroll
-            for (int j = 0; j < KJ; ++j) s = tree_mfma<BF>(k[j], q[j], s);
+                for (int u = 0; u < S::TT; ++u) s.t[u] = tree_mfma<BF, R>(k[u][j], q[j], s.t[u]);
             const int t0 = 32 * tile;
             const uint32_t there = (uint32_t)__ballot(row >= 0);   // (lanes 32 .. 63 repeat the tile's tokens)
             const bool more = tile + STEP < t_end;
@@ -407,67 +488,74 @@ __global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D)) void atten
                 page = tile + 2 * STEP < t_end ? page_at(tile + 2 * STEP) : -1;
             }
             // ---- tokens that are not there, and drafts that the lane's draft does not see
-            if (there != 0xFFFFFFFFu || t0 + 32 > pl.before || row0 + kRows > pl.count * t.G) {
+            if (there != 0xFFFFFFFFu || t0 + 32 > pl.before || row0 + R > pl.count * t.G) {
                 uint32_t bad = 0;   // drafts with a value that is not finite
                 if (t0 + 32 > pl.before) {
 #pragma unroll
-                    for (int u = 0; u < 16; ++u) {
+                    for (int u = 0; u < SN; ++u) {
                         bool b = false;
 #pragma unroll
                         for (int w = 0; w < VW; ++w) b |= any_nonfinite<BF>(x[u][w]);
                         const uint64_t lanes = __ballot(b);
-                        const int tok = 8 * (u >> 2) + (u & 3);
-                        if ((uint32_t)lanes) bad |= 1u << tok;
-                        if (lanes >> 32) bad |= 1u << (tok + 4);
+#pragma unroll
+                        for (int i = 0; i < S::LPR; ++i)
+                            if (lanes >> (R * i) & ((1ull << R) - 1)) bad |= 1u << (S::token_of(u) + 4 * i);
                     }
                     bad &= there & ~(pl.before > t0 ? (1u << (pl.before - t0)) - 1 : 0u);
                 }
                 const uint32_t kept = there & ~bad;
                 if (kept != 0xFFFFFFFFu) {   // their values are zeroed: a weight of 0 does not undo a NaN
 #pragma unroll
-                    for (int u = 0; u < 16; ++u) {
-                        const bool keep = (kept >> (8 * (u >> 2) + 4 * h + (u & 3))) & 1;
+                    for (int u = 0; u < SN; ++u) {
+                        const bool keep = (kept >> (S::token_of(u) + 4 * h)) & 1;
 #pragma unroll
                         for (int w = 0; w < VW; ++w) x[u][w] = keep ? x[u][w] : 0;
                     }
                 }
                 const uint32_t seen = seen_tokens(t, pl, draft, t0, there);
                 if (seen & bad) poison = NAN;
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (!((seen >> (8 * (i >> 2) + 4 * h + (i & 3))) & 1)) s[i] = -INFINITY;
+                hide_unseen<D, R>(s, seen, h);
             }
-            const Weights<BF> w = weigh<D, BF>(rows, s, t.qscale);
-            add_values<D, BF>(rows, x, w, 0);
-            add_values<D, BF>(rows, x + 8, w, 1);
+            const Weights<BF, R> w = weigh<D, BF, R>(rows, s, t.qscale);
+#pragma unroll
+            for (int part = 0; part < S::PARTS; ++part)
+#pragma unroll
+                for (int e = 0; e < MG; ++e) {
+                    tree_uint4 a;
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+                        a[y] = __builtin_amdgcn_perm(x[8 * part + 2 * y + 1][e >> 1], x[8 * part + 2 * y][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
+                    rows.acc[e] = tree_mfma<BF, R>(a, w.p[part], rows.acc[e]);
+                    if constexpr (BF) rows.acc[e] = tree_mfma<BF, R>(a, w.low[part], rows.acc[e]);
+                }
             if (more) load_values(next_row);
             row = next_row;
         }
         rows.l += poison;
     }
     if constexpr (!SHARE) {
-        store_rows<D, BF, false>(g, pl, rows, row0, lane);
+        store_rows<D, BF, R, false>(g, pl, rows, row0, lane);
     } else {
         // ---- the waves' shares
-        const float sum = other_half_sum(rows.l);
+        const float sum = row_sum<R>(rows.l);
         if (h == 0) m_s[wave][n] = sum == 0.0f ? -INFINITY : rows.m, l_s[wave][n] = sum;   // (no token: sum 0; else 1 at the least)
-        float* dst = o_s + (wave * kRows + n) * OSTRIDE;
+        float* dst = o_s + (wave * R + n) * OSTRIDE;
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
+        for (int q = 0; q < S::AN / 4; ++q)
 #pragma unroll
-            for (int c = 0; c < MG; ++c) {
+            for (int c = 0; c < 4 * MG; c += 4) {
                 float y[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] = rows.acc[(4 * c + i) % MG][4 * q + (4 * c + i) / MG];
-                *reinterpret_cast<float4*>(dst + MG * (8 * q + 4 * h) + 4 * c) = make_float4(y[0], y[1], y[2], y[3]);
+                for (int i = 0; i < 4; ++i) y[i] = rows.acc[(c + i) % MG][4 * q + (c + i) / MG];
+                *reinterpret_cast<float4*>(dst + 4 * MG * (S::LPR * q + h) + c) = make_float4(y[0], y[1], y[2], y[3]);
             }
         __syncthreads();
-        // eight threads of a row, each with D / 32 groups of four coordinates
-        const int rr = tid >> 3, part = tid & 7, r = row0 + rr;
+        // TPR threads of a row, each with groups of four coordinates in turn
+        constexpr int TPR = 256 / R, CG = D / (4 * TPR);
+        const int rr = tid / TPR, part = tid % TPR, r = row0 + rr;
         float M = m_s[0][rr];
 #pragma unroll
         for (int w = 1; w < 4; ++w) M = fmaxf(M, m_s[w][rr]);
-        const float own = M;
         float L = 0.0f, pool_M = -INFINITY, pool_L = 0.0f;
         const bool last = g.out != nullptr, with_pool = last && g.pool.ml != nullptr;
         const size_t stride = (size_t)v.A * t.rows, row = (size_t)pl.usel * g.pool.nsplit * stride + (size_t)pl.a * t.rows + min(r, t.rows - 1);
@@ -481,31 +569,34 @@ __global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D)) void atten
             f[w] = m_s[w][rr] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_s[w][rr] - M);
             L += l_s[w][rr] * f[w];
         }
-        float y[D / 8];
+        float y[4 * CG];
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) y[i] = 0.0f;
+        for (int i = 0; i < 4 * CG; ++i) y[i] = 0.0f;
         if (with_pool) {
             for (int s = 0; s < g.pool.nsplit; ++s) {
-                const float w = __builtin_amdgcn_exp2f(g.pool.ml[(row + s * stride) * 2] - M) *
-                                (g.pool.rotated ? (D == 64 ? 0.125f : D == 128 ? 0.08838834764831845f : 0.0625f) : 1.0f);
+                const float w = __builtin_amdgcn_exp2f(g.pool.ml[(row + s * stride) * 2] - M) * (g.pool.rotated ? kRotation(D) : 1.0f);
 #pragma unroll
-                for (int c = 0; c < MG; ++c) {
-                    const float4 z = *reinterpret_cast<const float4*>(g.pool.o + (row + s * stride) * D + 32 * c + 4 * part);
+                for (int c = 0; c < CG; ++c) {
+                    const float4 z = *reinterpret_cast<const float4*>(g.pool.o + (row + s * stride) * D + 4 * (TPR * c + part));
                     float* d = y + 4 * c;
                     d[0] = fmaf(z.x, w, d[0]), d[1] = fmaf(z.y, w, d[1]), d[2] = fmaf(z.z, w, d[2]), d[3] = fmaf(z.w, w, d[3]);
                 }
             }
             if (g.pool.rotated) {
-                wht_inlane<D / 8>(y);
+                wht_inlane<4 * CG>(y);
 #pragma unroll
-                for (int i = 0; i < D / 8; ++i) {
+                for (int i = 0; i < 4 * CG; ++i) {
                     y[i] = wht_lane_stage<1>(y[i], lane);
                     y[i] = wht_lane_stage<2>(y[i], lane);
                     y[i] = wht_lane_stage<4>(y[i], lane);
+                    if constexpr (TPR == 16) y[i] = wht_lane_stage<8>(y[i], lane);
                 }
                 if (g.pool.signs.on) {
 #pragma unroll
-                    for (int c = 0; c < MG; ++c) flip_signs<4>(*reinterpret_cast<float(*)[4]>(y + 4 * c), sign_word(g.pool.signs, c) >> (4 * part));
+                    for (int c = 0; c < CG; ++c) {
+                        const int at = 4 * (TPR * c + part);
+                        flip_signs<4>(*reinterpret_cast<float(*)[4]>(y + 4 * c), sign_word(g.pool.signs, at >> 5) >> (at & 31));
+                    }
                 }
             }
             L = fmaf(pool_L, __builtin_amdgcn_exp2f(pool_M - M), L);
@@ -513,19 +604,18 @@ __global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D)) void atten
         if (r >= t.rows) return;
         const float inv = L != 0.0f ? 1.0f / L : 0.0f;
         const size_t orow = out_row(g, pl, r), prow = partial_row(g, pl, r);
-        const bool any = own != -INFINITY || L != 0.0f;   // (a partial of no tokens: nobody reads its sums)
 #pragma unroll
-        for (int c = 0; c < MG; ++c) {
-            const int at = 32 * c + 4 * part;
+        for (int c = 0; c < CG; ++c) {
+            const int at = 4 * (TPR * c + part);
             float* d = y + 4 * c;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                const float4 z = *reinterpret_cast<const float4*>(o_s + (w * kRows + rr) * OSTRIDE + at);
+                const float4 z = *reinterpret_cast<const float4*>(o_s + (w * R + rr) * OSTRIDE + at);
                 d[0] = fmaf(z.x, f[w], d[0]), d[1] = fmaf(z.y, f[w], d[1]), d[2] = fmaf(z.z, f[w], d[2]), d[3] = fmaf(z.w, f[w], d[3]);
             }
             if (last)
                 *reinterpret_cast<uint2*>(g.out + orow * D + at) = make_uint2(pack2<BF>(d[0] * inv, d[1] * inv), pack2<BF>(d[2] * inv, d[3] * inv));
-            else if (any)
+            else if (L != 0.0f)   // (a partial of no tokens: nobody reads its sums)
                 *reinterpret_cast<float4*>(g.o + prow * D + at) = make_float4(d[0], d[1], d[2], d[3]);
         }
         if (!last && part == 0) *reinterpret_cast<float2*>(g.ml + prow * 2) = make_float2(M, L);
@@ -538,6 +628,7 @@ __global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D)) void atten
 // fetches for the tile after the next waits in registers until the tile before is done with.  (Keys straight from the pages as
 // operands, as above, are 32-byte pieces of 32 rows per load: four waves that fetch the same tile that way are bound by the L1.)
 template <int I> using Set = std::integral_constant<int, I>;
+constexpr int kRows = 32;   // rows of a wave
 constexpr int many_waves_per_simd(int D) { return D == 256 ? 1 : 2; }
 
 template <int D, bool BF, int W>
@@ -607,7 +698,7 @@ __global__ __launch_bounds__(64 * W, many_waves_per_simd(D)) void attend_pages_m
         }
     };
 
-    Rows<D> rows;
+    Rows<D, kRows> rows;
     rows.clear();
     if (t_begin < t_end) {   // (the same for all waves)
         // Tile t_begin + i waits for LDS in register set i % SETS.
@@ -620,32 +711,30 @@ __global__ __launch_bounds__(64 * W, many_waves_per_simd(D)) void attend_pages_m
         if constexpr (SETS > 1) ask(t_begin + 1, Set<1 % SETS>());
         if constexpr (SETS > 2) ask(t_begin + 2, Set<2 % SETS>());
         tree_uint4 q[KJ];
-        const int draft = load_queries<D>(g, pl, my_row0, lane, q);
+        const int draft = load_queries<D, kRows>(g, pl, my_row0, lane, q);
         float poison = 0.0f;
         if (draft >= pl.count) rows.m = 0.0f;   // such a row never sees a token: any reference will do
         stage(t_begin, Set<0>());
-        wait_for<D>(q);
+        wait_for(q);
         ask(t_begin + SETS, Set<0>());
         __syncthreads();
 
         auto step = [&](int tile, auto next) {   // `next`: the set with the tile behind it
             uint16_t* const src = kv_s + (tile & 1) * TILE;
             const int t0 = 32 * tile;
-            tree_float16 s;
+            Scores<kRows> s;
+            s.clear();
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = 0.0f;
-#pragma unroll
-            for (int j = 0; j < KJ; ++j) s = tree_mfma<BF>(*reinterpret_cast<const tree_uint4*>(src + n * KS + 16 * j + 8 * h), q[j], s);
+            for (int j = 0; j < KJ; ++j)
+                s.t[0] = tree_mfma<BF, kRows>(*reinterpret_cast<const tree_uint4*>(src + n * KS + 16 * j + 8 * h), q[j], s.t[0]);
             const int flags = flag_s[tile & 1][n];
             const uint32_t there = (uint32_t)__ballot(flags & 1);
             if (there != 0xFFFFFFFFu || t0 + 32 > pl.before || my_row0 + kRows > pl.count * t.G) {
                 const uint32_t bad = (uint32_t)__ballot(flags & 2), seen = seen_tokens(t, pl, draft, t0, there);
                 if (seen & bad) poison = NAN;
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (!((seen >> (8 * (i >> 2) + 4 * h + (i & 3))) & 1)) s[i] = -INFINITY;
+                hide_unseen<D, kRows>(s, seen, h);
             }
-            const Weights<BF> w = weigh<D, BF>(rows, s, t.qscale);
+            const Weights<BF, kRows> w = weigh<D, BF, kRows>(rows, s, t.qscale);
             // values: sixteen lanes read 16 coordinates of four tokens and get four tokens of one coordinate each
             uint16_t* const vals = src + 32 * KS + (4 * h + ((lane & 15) >> 2)) * VS + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
 #pragma unroll
@@ -654,8 +743,8 @@ __global__ __launch_bounds__(64 * W, many_waves_per_simd(D)) void attend_pages_m
                 for (int e = 0; e < MG; ++e) {
                     const uint2 lo = lds_transposed(vals + 16 * half * VS + 32 * e), hi = lds_transposed(vals + (16 * half + 8) * VS + 32 * e);
                     const tree_uint4 a = {lo.x, lo.y, hi.x, hi.y};
-                    rows.acc[e] = tree_mfma<BF>(a, w.p[half], rows.acc[e]);
-                    if constexpr (BF) rows.acc[e] = tree_mfma<BF>(a, w.low[half], rows.acc[e]);
+                    rows.acc[e] = tree_mfma<BF, kRows>(a, w.p[half], rows.acc[e]);
+                    if constexpr (BF) rows.acc[e] = tree_mfma<BF, kRows>(a, w.low[half], rows.acc[e]);
                 }
             if (tile + 1 < t_end) {
                 stage(tile + 1, next);
@@ -672,7 +761,7 @@ __global__ __launch_bounds__(64 * W, many_waves_per_simd(D)) void attend_pages_m
         }
         rows.l += poison;
     }
-    store_rows<D, BF, true>(g, pl, rows, my_row0, lane);
+    store_rows<D, BF, kRows, true>(g, pl, rows, my_row0, lane);
 }
 
 // -------------------------------------------------------------------------------------- merge ---
@@ -743,10 +832,12 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(AttendPlan p, int nspli
 void plan_tree(const PageView& v, int page_splits, TreePlan* t) {
     const int row_tiles = (t->rows + kRows - 1) / kRows;
     const long tiles = ((long)v.max_blocks * v.P + 31) / 32, units = (long)t->layers * v.H * v.A;
-    t->waves = row_tiles > 2 ? 4 : row_tiles;
+    t->wave_rows = t->rows <= 16 || v.D == 256 ? 16 : 32;
+    t->waves = row_tiles > 2 ? 4 : v.D == 256 && t->rows > 16 ? 2 : row_tiles;
     t->share = units * row_tiles <= 512 ? 1 : 0;
     if (t->share) t->waves = 1;
-    const int rows = kRows * t->waves;
+    if (t->waves > 1) t->wave_rows = 32;
+    const int rows = t->wave_rows * t->waves;
     t->row_blocks = (t->rows + rows - 1) / rows;
     // Token ranges: workgroups for 512 places, as far as each of a workgroup's four waves keeps two tiles of the longest
     // continuation there can be.
@@ -775,11 +866,12 @@ struct PagesForm {
     int threads, shared;
 };
 template <int D, bool BF> static PagesForm pages_form(const TreePlan& t) {
-    constexpr int kShare = 4 * kRows * (D + 4) * (int)sizeof(float), kStage = 2 * 32 * (2 * D + 40) * (int)sizeof(uint16_t);
+    constexpr int kShare = 4 * (D + 4) * (int)sizeof(float), kStage = 2 * 32 * (2 * D + 40) * (int)sizeof(uint16_t);
     if (t.waves == 4) return {attend_pages_many_kernel<D, BF, 4>, 256, kStage};
     if (t.waves == 2) return {attend_pages_many_kernel<D, BF, 2>, 128, kStage};
-    if (t.share) return {attend_pages_few_kernel<D, BF, true>, 256, kShare};
-    return {attend_pages_few_kernel<D, BF, false>, 64, 0};
+    if constexpr (D != 256)
+        if (t.wave_rows == 32) return t.share ? PagesForm{attend_pages_few_kernel<D, BF, 32, true>, 256, 32 * kShare} : PagesForm{attend_pages_few_kernel<D, BF, 32, false>, 64, 0};
+    return t.share ? PagesForm{attend_pages_few_kernel<D, BF, 16, true>, 256, 16 * kShare} : PagesForm{attend_pages_few_kernel<D, BF, 16, false>, 64, 0};
 }
 
 hipError_t launch_attend_pages(const PageView& v, const TreePlan& t, bool bf16, const void* Q, float* ml, float* o, void* out,

@@ -573,12 +573,10 @@ class Pages:
             if rc != ENOMEM or not own:
                 _check(rc)
                 return out
-        need = lib.pool_attend_tree_workspace(pool, self._ref, ref)
-        if need:
-            ws = _new((need,), torch.uint8, device, stream)
-            if not capturing:
-                self._workspaces[sp] = ws
-            p.workspace_dev, p.workspace_bytes = ws.data_ptr(), need
+        ws = _new((max(lib.pool_attend_tree_workspace(pool, self._ref, ref), 256),), torch.uint8, device, stream)
+        if not capturing:
+            self._workspaces[sp] = ws
+        p.workspace_dev, p.workspace_bytes = ws.data_ptr(), ws.numel()
         _check(lib.pool_attend_tree(pool, self._ref, q_ptr, out_ptr, ref, sp))
         return out
 
