@@ -288,6 +288,7 @@ typedef struct {
     int32_t* lengths_dev;           /* [agents]: tokens in an agent's pages                                     */
     int32_t* free_dev;              /* [pages]: ring of the free pages' numbers (polykv_pages_resize only)      */
     int32_t* free_state_dev;        /* [2]: place of the first free page in the ring, and how many there are    */
+    int32_t* ticket_dev;            /* [1]: 0 before polykv_pages_resize, which leaves it 0                     */
 } polykv_pages;
 
 /* Block tables and slot maps from lengths: agent a's continuation becomes targets_dev[a] tokens long.  With

@@ -12,9 +12,8 @@
 namespace polykv {
 
 // ------------------------------------------------------------------------------- block tables ---
-// Inclusive sums over the threads of a workgroup (1,024 of them) of three numbers at once; `total` is the whole
-// workgroup's.  The first is capped: it is only compared with the number of free pages, and the sum of what 4,096 agents
-// may ask for does not fit 32 bits.
+// Sums over agents of three numbers at once.  The first is capped: it is only compared with the number of free pages, and
+// the sum of what 4,096 agents may ask for does not fit 32 bits.
 constexpr uint32_t kNeedCap = 1u << 28;   // above every page number
 struct Sums {
     uint32_t need, give, grow;
@@ -51,23 +50,22 @@ __device__ __forceinline__ AgentChange change_of(const PageView& v, const int32_
     return c;
 }
 
-constexpr int kResizeThreads = 1024;
-
 // Every workgroup works out the sums over all agents for itself -- 4,096 agents are four rounds -- and then does its share of
 // the agents' table entries and of the slots, the agent of a slot by bisection.  Nothing that other workgroups still read is
-// written: the lengths and the ring's state follow in a launch of one workgroup (COMMIT), or, where a step is small, one
-// workgroup does everything in one launch (FILL and COMMIT).  Pages that are given back go behind the ring's last, where no
-// page to be taken lies, so the two do not have to wait for each other.
-template <bool FILL, bool COMMIT>
-__global__ __launch_bounds__(kResizeThreads) void pages_resize_kernel(PageView v, const int32_t* __restrict__ targets, int32_t* ring,
-                                                                      int32_t* state, int32_t* __restrict__ slots, int n_slots,
+// written before they are done: the workgroup that is the last to say so writes the lengths and the ring's state (nobody waits
+// for anybody; a launch of its own for them took 4.5 us).  Pages that are given back go behind the ring's last, where no page to
+// be taken lies, so the two do not have to wait for each other.
+// A step of few agents is all latency: 256 threads there (15 agents, 195 slots: 4.5 us, with 1,024 threads 5.2).
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void pages_resize_kernel(PageView v, const int32_t* __restrict__ targets, int32_t* ring,
+                                                                      int32_t* state, int32_t* ticket, int32_t* __restrict__ slots, int n_slots,
                                                                       int32_t* __restrict__ offsets) {
     extern __shared__ int shared[];
     int* const end_s = shared;                 // where an agent's new tokens end in the slot map
     int* const len_s = shared + v.A;           // its length
     int* const tgt_s = shared + 2 * v.A;       // its length after the call
     int* const at_s = shared + 3 * v.A;        // its first page among those taken, or given back
-    __shared__ Sums wave_s[kResizeThreads / 64];
+    __shared__ Sums wave_s[THREADS / 64];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const uint32_t NP = v.pages;
@@ -76,7 +74,7 @@ __global__ __launch_bounds__(kResizeThreads) void pages_resize_kernel(PageView v
     const uint32_t count = min((uint32_t)max(state[1], 0), NP);
     Sums before = {0, 0, 0};
     uint32_t taken = 0;
-    for (int a0 = 0; a0 < v.A; a0 += kResizeThreads) {
+    for (int a0 = 0; a0 < v.A; a0 += THREADS) {
         const int a = a0 + tid;
         AgentChange c = change_of(v, targets, a);
         // what is asked for, whether it is there, and only then what the slots are
@@ -87,7 +85,7 @@ __global__ __launch_bounds__(kResizeThreads) void pages_resize_kernel(PageView v
         if (lane == 63) wave_s[wave] = sum;
         __syncthreads();
         Sums base = before, total = before;
-        for (int w = 0; w < kResizeThreads / 64; ++w) {
+        for (int w = 0; w < THREADS / 64; ++w) {
             if (w == wave) base = total;
             total = add(total, wave_s[w]);
         }
@@ -105,7 +103,7 @@ __global__ __launch_bounds__(kResizeThreads) void pages_resize_kernel(PageView v
         if (lane == 63) wave_s[wave] = Sums{most, 0u, g.grow};
         __syncthreads();
         uint32_t grow_base = before.grow, grow_total = before.grow;
-        for (int w = 0; w < kResizeThreads / 64; ++w) {
+        for (int w = 0; w < THREADS / 64; ++w) {
             if (w == wave) grow_base = grow_total;
             grow_total += wave_s[w].grow;
             taken = max(taken, wave_s[w].need);
@@ -122,53 +120,66 @@ __global__ __launch_bounds__(kResizeThreads) void pages_resize_kernel(PageView v
     __syncthreads();
     const int grown = v.A > 0 ? end_s[v.A - 1] : 0;
 
-    if constexpr (FILL) {
-        const int waves = gridDim.x * (kResizeThreads / 64);
-        for (int a = blockIdx.x * (kResizeThreads / 64) + wave; a < v.A; a += waves) {
+    const int waves = gridDim.x * (THREADS / 64);
+    for (int a = blockIdx.x * (THREADS / 64) + wave; a < v.A; a += waves) {
+        int rem;
+        int have = v.div_P.divide(len_s[a], &rem);
+        have += rem > 0;
+        int want = v.div_P.divide(tgt_s[a], &rem);
+        want += rem > 0;
+        int32_t* row = v.table + (size_t)a * v.max_blocks;
+        for (int b = have + lane; b < want; b += 64) row[b] = ring[(first + (uint32_t)at_s[a] + (uint32_t)(b - have)) % NP];
+        for (int b = want + lane; b < have; b += 64) {
+            ring[(first + count + (uint32_t)at_s[a] + (uint32_t)(b - want)) % NP] = row[b];
+            row[b] = -1;
+        }
+    }
+    // four slots of a thread: one bisection, and then on from agent to agent
+    for (int i0 = 4 * (blockIdx.x * THREADS + tid); i0 < n_slots; i0 += 4 * gridDim.x * THREADS) {
+        int a = 0;
+        if (i0 < grown) {   // the first agent whose tokens end behind i0
+            int hi = v.A - 1;
+            while (a < hi) {
+                const int mid = (a + hi) >> 1;
+                if (end_s[mid] > i0) hi = mid;
+                else a = mid + 1;
+            }
+        }
+        int page[4], off[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            page[u] = -1, off[u] = 0;
+            const int i = i0 + u;
+            if (i >= grown) continue;
+            while (a < v.A - 1 && end_s[a] <= i) ++a;
             int rem;
             int have = v.div_P.divide(len_s[a], &rem);
             have += rem > 0;
-            int want = v.div_P.divide(tgt_s[a], &rem);
-            want += rem > 0;
-            int32_t* row = v.table + (size_t)a * v.max_blocks;
-            for (int b = have + lane; b < want; b += 64) row[b] = ring[(first + (uint32_t)at_s[a] + (uint32_t)(b - have)) % NP];
-            for (int b = want + lane; b < have; b += 64) {
-                ring[(first + count + (uint32_t)at_s[a] + (uint32_t)(b - want)) % NP] = row[b];
-                row[b] = -1;
-            }
+            // (in range for whatever the sums hold)
+            const int t = min(max(tgt_s[a] - (end_s[a] - i), 0), v.max_blocks * v.P - 1);
+            const int b = v.div_P.divide(t, &off[u]);
+            page[u] = b < have ? v.table[(size_t)a * v.max_blocks + b] : ring[(first + (uint32_t)at_s[a] + (uint32_t)(b - have)) % NP];
         }
-        for (int i = blockIdx.x * kResizeThreads + tid; i < n_slots; i += gridDim.x * kResizeThreads) {
-            int slot = -1;
-            if (i < grown) {
-                int lo = 0, hi = v.A - 1;   // the first agent whose tokens end behind i
-                while (lo < hi) {
-                    const int mid = (lo + hi) >> 1;
-                    if (end_s[mid] > i) hi = mid;
-                    else lo = mid + 1;
-                }
-                int rem, off;
-                int have = v.div_P.divide(len_s[lo], &rem);
-                have += rem > 0;
-                // (in range for whatever the sums hold)
-                const int t = min(max(tgt_s[lo] - (end_s[lo] - i), 0), v.max_blocks * v.P - 1);
-                const int b = v.div_P.divide(t, &off);
-                const int page = b < have ? v.table[(size_t)lo * v.max_blocks + b]
-                                          : ring[(first + (uint32_t)at_s[lo] + (uint32_t)(b - have)) % NP];
-                if ((uint32_t)page < NP) slot = page * v.P + off;
-            }
-            slots[i] = slot;
-        }
-        if (offsets != nullptr && blockIdx.x == 0) {
-            for (int a = tid; a < v.A; a += kResizeThreads) offsets[a + 1] = end_s[a];
-            if (tid == 0) offsets[0] = 0;
-        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (i0 + u < n_slots) slots[i0 + u] = (uint32_t)page[u] < NP ? page[u] * v.P + off[u] : -1;
     }
-    if constexpr (COMMIT) {
-        for (int a = tid; a < v.A; a += kResizeThreads) v.lengths[a] = tgt_s[a];
-        if (tid == 0) {
-            state[0] = (int)((first + taken) % NP);
-            state[1] = (int)min(count - min(taken, count) + before.give, NP);
-        }
+    if (offsets != nullptr && blockIdx.x == 0) {
+        for (int a = tid; a < v.A; a += THREADS) offsets[a + 1] = end_s[a];
+        if (tid == 0) offsets[0] = 0;
+    }
+    __shared__ int last_s;
+    if (gridDim.x > 1) {   // (what this workgroup has read of lengths and state is in LDS and registers by now)
+        __syncthreads();
+        if (tid == 0) last_s = atomicAdd(ticket, 1) == (int)gridDim.x - 1;
+        __syncthreads();
+        if (!last_s) return;
+        if (tid == 0) *ticket = 0;
+    }
+    for (int a = tid; a < v.A; a += THREADS) v.lengths[a] = tgt_s[a];
+    if (tid == 0) {
+        state[0] = (int)((first + taken) % NP);
+        state[1] = (int)min(count - min(taken, count) + before.give, NP);
     }
 }
 
@@ -179,26 +190,19 @@ hipError_t launch_pages_resize(const polykv_pages* p, const int32_t* targets, in
     static std::once_flag configured;
     static hipError_t config_result = hipSuccess;
     std::call_once(configured, []() {
-        for (auto kern : {pages_resize_kernel<true, true>, pages_resize_kernel<true, false>, pages_resize_kernel<false, true>})
-            if (config_result == hipSuccess)
-                config_result = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                    4 * POLYKV_MAX_PAGED_AGENTS * (int)sizeof(int));
+        config_result = hipFuncSetAttribute(reinterpret_cast<const void*>(pages_resize_kernel<1024>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                            4 * POLYKV_MAX_PAGED_AGENTS * (int)sizeof(int));
     });
     if (config_result != hipSuccess) return config_result;
     if (slots == nullptr) n_slots = 0;
-    if (v.A <= 64 && n_slots <= 4 * kResizeThreads) {
-        launch_kernel(pages_resize_kernel<true, true>, dim3(1), dim3(kResizeThreads), shared, s, {}, v, targets, p->free_dev,
-                      p->free_state_dev, slots, n_slots, offsets);
-        return hipGetLastError();
+    if (v.A <= 64 && n_slots <= 4096) {
+        launch_kernel(pages_resize_kernel<256>, dim3(1), dim3(256), shared, s, {}, v, targets, p->free_dev, p->free_state_dev, p->ticket_dev, slots,
+                      n_slots, offsets);
+    } else {
+        const int by_slots = (n_slots + 4095) / 4096, by_agents = (v.A + 15) / 16;   // a round each: four slots a thread, an agent a wave
+        launch_kernel(pages_resize_kernel<1024>, dim3(min(max(by_slots, by_agents), 256)), dim3(1024), shared, s, {}, v, targets, p->free_dev,
+                      p->free_state_dev, p->ticket_dev, slots, n_slots, offsets);
     }
-    const int by_slots = (n_slots + kResizeThreads - 1) / kResizeThreads, by_agents = (v.A + kResizeThreads / 64 - 1) / (kResizeThreads / 64);
-    const int groups = min(max(by_slots, by_agents), 256);
-    launch_kernel(pages_resize_kernel<true, false>, dim3(groups), dim3(kResizeThreads), shared, s, {}, v, targets, p->free_dev,
-                  p->free_state_dev, slots, n_slots, offsets);
-    hipError_t err = hipGetLastError();
-    if (err != hipSuccess) return err;
-    launch_kernel(pages_resize_kernel<false, true>, dim3(1), dim3(kResizeThreads), shared, s, {}, v, targets, p->free_dev,
-                  p->free_state_dev, nullptr, 0, nullptr);
     return hipGetLastError();
 }
 
@@ -315,8 +319,8 @@ hipError_t launch_tree_masks(const int32_t* parents, const int32_t* counts, int 
 
 // One workgroup per agent and layer; each works the path out for itself (the layers' first writes it down).
 // A draft that continues its parent as the model does enters itself as the parent's successor, the lowest one stays, and the
-// path follows the successors from draft 0.  Then a thread moves one 16-byte piece of one head's keys or values along the whole
-// path: a path's k-th draft is k at the least, so what is read for step k lies behind everything written before it, and
+// path follows the successors from draft 0.  Then a thread moves one 16-byte piece of one head's keys, and of its values, along the
+// whole path: a path's k-th draft is k at the least, so what is read for step k lies behind everything written before it, and
 // eight steps' pieces are read before they are written.
 __global__ __launch_bounds__(256) void pages_accept_kernel(PageView v, const int32_t* __restrict__ tokens, const int32_t* __restrict__ following,
                                                            const int32_t* __restrict__ parents, const int32_t* __restrict__ counts,
@@ -361,18 +365,25 @@ __global__ __launch_bounds__(256) void pages_accept_kernel(PageView v, const int
     __syncthreads();
     const int pieces = v.H * v.D / 8, per_head = v.D / 8;
     const size_t layer = (size_t)l * v.pages * v.H * v.P * v.D;
-    for (int item = i; item < 2 * pieces; item += 256) {
-        const int piece = item < pieces ? item : item - pieces;
+    for (int piece = i; piece < pieces; piece += 256) {
         const int h = piece / per_head;
-        uint16_t* const base = (item < pieces ? v.K : v.V) + layer + (size_t)h * v.P * v.D + (piece - h * per_head) * 8;
+        const size_t at_head = layer + (size_t)h * v.P * v.D + (piece - h * per_head) * 8;
         for (int k0 = 1; k0 < n; k0 += 8) {
-            page_uint4 x[8];
+            page_uint4 x[8], y[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-                if (k0 + k < n && from_s[k0 + k] >= 0) x[k] = *reinterpret_cast<const page_uint4*>(base + (size_t)from_s[k0 + k] * v.D);
+                if (k0 + k < n && from_s[k0 + k] >= 0) {
+                    const size_t from = at_head + (size_t)from_s[k0 + k] * v.D;
+                    x[k] = *reinterpret_cast<const page_uint4*>(v.K + from);
+                    y[k] = *reinterpret_cast<const page_uint4*>(v.V + from);
+                }
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-                if (k0 + k < n && to_s[k0 + k] >= 0) *reinterpret_cast<page_uint4*>(base + (size_t)to_s[k0 + k] * v.D) = x[k];
+                if (k0 + k < n && from_s[k0 + k] >= 0) {
+                    const size_t to = at_head + (size_t)to_s[k0 + k] * v.D;
+                    *reinterpret_cast<page_uint4*>(v.K + to) = x[k];
+                    *reinterpret_cast<page_uint4*>(v.V + to) = y[k];
+                }
         }
     }
 }

@@ -7,6 +7,7 @@
 #include <hip/hip_bf16.h>
 #include <hip/hip_fp16.h>
 
+#include <algorithm>
 #include <mutex>
 #include <type_traits>
 
@@ -778,22 +779,46 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(AttendPlan p, int nspli
     const int usel = (int)(rg / p.R), r = (int)(rg - (long)usel * p.R);
     int kvh;
     const int ls = p.div_H.divide(usel, &kvh);
-    // (m, l) of a partial, from every lane: the numbers are the same for the whole wave
-    auto pool_at = [&](int s) { return *reinterpret_cast<const float2*>(pool_ml + (((size_t)usel * nsplit + s) * p.R + r) * 2); };
-    auto page_at = [&](int s) { return *reinterpret_cast<const float2*>(ml + (((size_t)usel * page_nsplit + s) * p.R + r) * 2); };
+    // Lane s holds (m, l) of split s: first the maximum over all splits, then sixty-four splits' weights at a time, which are handed
+    // out with readlane; eight partial rows are requested at once.
+    auto sums_of = [&](const float* base, int n, int s) {
+        return s < n ? *reinterpret_cast<const float2*>(base + (((size_t)usel * n + s) * p.R + r) * 2) : make_float2(-INFINITY, 0.0f);
+    };
     float M = -INFINITY;
-    for (int s = 0; s < nsplit; ++s) M = fmaxf(M, pool_at(s).x);
-    for (int s = 0; s < page_nsplit; ++s) M = fmaxf(M, page_at(s).x);
+    for (int s0 = 0; s0 < nsplit; s0 += 64) M = fmaxf(M, sums_of(pool_ml, nsplit, s0 + lane).x);
+    for (int s0 = 0; s0 < page_nsplit; s0 += 64) M = fmaxf(M, sums_of(ml, page_nsplit, s0 + lane).x);
+    M = fmaxf(M, lane_xor<1>(M));
+    M = fmaxf(M, lane_xor<2>(M));
+    M = fmaxf(M, lane_xor<4>(M));
+    M = fmaxf(M, lane_xor<8>(M));
+    M = row_max<16>(M);
     float x[EPL], L = 0.0f;
 #pragma unroll
     for (int i = 0; i < EPL; ++i) x[i] = 0.0f;
-    for (int s = 0; s < nsplit; ++s) {
-        const float2 part = pool_at(s);
-        const float w = part.x == -INFINITY ? 0.0f : exp2f(part.x - M);
-        L = fmaf(part.y, w, L);
+    auto add = [&](const float* base_ml, const float* base_o, int n) {
+        for (int s0 = 0; s0 < n; s0 += 64) {
+            const float2 part = sums_of(base_ml, n, s0 + lane);
+            const float w = part.x == -INFINITY ? 0.0f : exp2f(part.x - M);   // (a partial of no tokens)
+            L = fmaf(part.y, w, L);
+            const int cnt = min(64, n - s0);
+            const float* src = base_o + (((size_t)usel * n + s0) * p.R + r) * D + lane * EPL;
+            for (int k0 = 0; k0 < cnt; k0 += 8) {
+                float v[8][EPL], wk[8];
 #pragma unroll
-        for (int i = 0; i < EPL; ++i) x[i] = fmaf(pool_o[(((size_t)usel * nsplit + s) * p.R + r) * D + lane * EPL + i], w, x[i]);
-    }
+                for (int k = 0; k < 8; ++k) {
+                    wk[k] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), min(k0 + k, 63)));
+                    const bool used = k0 + k < cnt && wk[k] != 0.0f;   // (sums that weigh nothing need not have been written)
+#pragma unroll
+                    for (int i = 0; i < EPL; ++i) v[k][i] = used ? src[(size_t)(k0 + k) * p.R * D + i] : 0.0f;
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+#pragma unroll
+                    for (int i = 0; i < EPL; ++i) x[i] = fmaf(v[k][i], wk[k], x[i]);
+            }
+        }
+    };
+    add(pool_ml, pool_o, nsplit);
     if (nsplit > 0 && p.vcodec != POLYKV_VALUES_INT8) {   // (int8 values were never rotated)
         wht_inlane<EPL>(x);
 #pragma unroll
@@ -808,14 +833,12 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(AttendPlan p, int nspli
         }
         if (p.signs.on) flip_signs<EPL>(x, sign_word(p.signs, (lane * EPL) >> 5) >> ((lane * EPL) & 31));
     }
-    for (int s = 0; s < page_nsplit; ++s) {
-        const float2 part = page_at(s);
-        if (part.x == -INFINITY && part.y == 0.0f) continue;   // no token: its sums were not written
-        const float w = exp2f(part.x - M);
-        L = fmaf(part.y, w, L);
-#pragma unroll
-        for (int i = 0; i < EPL; ++i) x[i] = fmaf(o[(((size_t)usel * page_nsplit + s) * p.R + r) * D + lane * EPL + i], w, x[i]);
-    }
+    add(ml, o, page_nsplit);
+    L += lane_xor<1>(L);
+    L += lane_xor<2>(L);
+    L += lane_xor<4>(L);
+    L += lane_xor<8>(L);
+    L = row_sum<16>(L);
     const float inv = L != 0.0f ? 1.0f / L : 0.0f;
     if (active) {
         uint16_t* dst = out + q_row_index(p, ls, kvh, r) * D + lane * EPL;
@@ -832,20 +855,32 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(AttendPlan p, int nspli
 void plan_tree(const PageView& v, int page_splits, TreePlan* t) {
     const int row_tiles = (t->rows + kRows - 1) / kRows;
     const long tiles = ((long)v.max_blocks * v.P + 31) / 32, units = (long)t->layers * v.H * v.A;
-    t->wave_rows = t->rows <= 16 || v.D == 256 ? 16 : 32;
-    t->waves = row_tiles > 2 ? 4 : v.D == 256 && t->rows > 16 ? 2 : row_tiles;
     t->share = units * row_tiles <= 512 ? 1 : 0;
-    if (t->share) t->waves = 1;
-    if (t->waves > 1) t->wave_rows = 32;
+    t->wave_rows = t->rows <= 16 || v.D == 256 ? 16 : 32;
+    t->waves = 1;
+    if (!t->share && (row_tiles > 1 || (v.D == 256 && t->rows > 16))) {
+        t->wave_rows = 32;
+        t->waves = 2;
+        if ((row_tiles + 3) / 4 * 4 <= (row_tiles + 1) / 2 * 2) t->waves = 4;
+    }
     const int rows = t->wave_rows * t->waves;
     t->row_blocks = (t->rows + rows - 1) / rows;
-    // Token ranges: workgroups for 512 places, as far as each of a workgroup's four waves keeps two tiles of the longest
-    // continuation there can be.
     const long groups = units * t->row_blocks;
-    long want = page_splits > 0 ? page_splits : (512 + groups - 1) / groups;
-    const long most = page_splits > 0 ? (tiles + 3) / 4 : tiles / 8;
-    if (want > most) want = most;
-    if (want < 1) want = 1;
+    // Token ranges: the count with the least estimated time, in steps of a wave (one tile): rounds of workgroups over the places
+    // there are, times the steps of the longest continuation there can be plus four for the ramp and the final pass; more than
+    // one range adds the merge kernel and the partials.
+    const int wave_places = v.D == 256 ? 8 : t->wave_rows == 32 && t->waves == 1 ? (v.D == 64 ? 12 : 8) : t->waves > 1 ? 8 : v.D == 64 ? 16 : 12;
+    const int ways = t->share ? 4 : 1;
+    const long places = 256l * (wave_places / (t->share ? 4 : t->waves));
+    long want = 1, most = std::min((tiles + 3) / 4, 64l);
+    auto cost = [&](long n) {
+        const double steps = (double)((tiles + n * ways - 1) / (n * ways)) + 4;
+        const double rounds = (double)((groups * n + places - 1) / places);
+        return rounds * steps + (n > 1 ? 6 + n * (double)units * t->rows * v.D * (8 / 4e12 / 1.5e-6) : 0.0);
+    };
+    for (long n = 2; n <= most; ++n)
+        if (cost(n) < cost(want)) want = n;
+    if (page_splits > 0) want = std::min((long)page_splits, (tiles + 3) / 4);
     t->nsplit = (int)want;
     t->div_H = FastDiv::by(v.H);
     t->div_A = FastDiv::by(v.A);

@@ -135,11 +135,11 @@ int polykv_pages_resize(const polykv_pages* pages, const int32_t* targets_dev, i
     const char* who = "polykv_pages_resize";
     const int rc = check_pages(pages, false, who);
     if (rc != POLYKV_OK) return rc;
-    if (pages->free_dev == nullptr || pages->free_state_dev == nullptr || targets_dev == nullptr) {
-        set_error("%s: NULL free list or targets", who);
+    if (pages->free_dev == nullptr || pages->free_state_dev == nullptr || pages->ticket_dev == nullptr || targets_dev == nullptr) {
+        set_error("%s: NULL free list, ticket or targets", who);
         return POLYKV_EINVAL;
     }
-    if (!aligned(pages->free_dev, 4) || !aligned(pages->free_state_dev, 4) || !aligned(targets_dev, 4) || !aligned(slots_dev, 4) ||
+    if (!aligned(pages->free_dev, 4) || !aligned(pages->free_state_dev, 4) || !aligned(pages->ticket_dev, 4) || !aligned(targets_dev, 4) || !aligned(slots_dev, 4) ||
         !aligned(offsets_dev, 4)) {
         set_error("%s: arrays must be 4-byte aligned", who);
         return POLYKV_EINVAL;

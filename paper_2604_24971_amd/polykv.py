@@ -50,7 +50,7 @@ class AttendChoice(C.Structure):
 
 class PagesDesc(C.Structure):
     _fields_ = [(n, C.c_int) for n in ("layers", "kv_heads", "head_dim", "pages", "page_tokens", "agents", "max_blocks", "dtype")] + \
-        [(n, C.c_void_p) for n in ("K_dev", "V_dev", "table_dev", "lengths_dev", "free_dev", "free_state_dev")]
+        [(n, C.c_void_p) for n in ("K_dev", "V_dev", "table_dev", "lengths_dev", "free_dev", "free_state_dev", "ticket_dev")]
 
 
 class TreeParams(C.Structure):
@@ -482,8 +482,10 @@ class Pages:
         self.lengths = torch.zeros((agents,), dtype=torch.int32, device=self.device)
         self.free = torch.arange(pages, dtype=torch.int32, device=self.device)
         self.free_state = torch.tensor([0, pages], dtype=torch.int32, device=self.device)
+        self._ticket = torch.zeros((1,), dtype=torch.int32, device=self.device)
         self._desc = PagesDesc(layers, kv_heads, head_dim, pages, page_tokens, agents, max_blocks, _DTYPES[dtype],
-                               *(t.data_ptr() for t in (self.K, self.V, self.table, self.lengths, self.free, self.free_state)))
+                               *(t.data_ptr() for t in (self.K, self.V, self.table, self.lengths, self.free, self.free_state,
+                                                         self._ticket)))
         self._ref = C.byref(self._desc)
         self._index = self.device.index
         self._per_agent, self._per_offset = self.lengths.shape, torch.Size((agents + 1,))

@@ -10,7 +10,7 @@ P = C.c_void_p(0x10000)      # never dereferenced: every call below ends before 
 
 def desc(**kw):
     d = dict(layers=2, kv_heads=2, head_dim=64, pages=10, page_tokens=16, agents=3, max_blocks=4, dtype=pk.F16, K_dev=P, V_dev=P,
-             table_dev=P, lengths_dev=0x20000, free_dev=P, free_state_dev=P)
+             table_dev=P, lengths_dev=0x20000, free_dev=P, free_state_dev=P, ticket_dev=P)
     d.update(kw)
     return pk.PagesDesc(**{k: getattr(v, "value", v) for k, v in d.items()})
 
@@ -65,6 +65,7 @@ def test_resize_refusals():
     assert f(d, P, P, 2 ** 30 + 1, P, None) == pk.ESHAPE
     assert f(C.byref(desc(free_dev=None)), P, P, 10, P, None) == pk.EINVAL
     assert f(C.byref(desc(free_state_dev=None)), P, P, 10, P, None) == pk.EINVAL
+    assert f(C.byref(desc(ticket_dev=None)), P, P, 10, P, None) == pk.EINVAL
 
 
 def test_write_refusals():
