@@ -155,26 +155,29 @@ template <int N> __device__ __forceinline__ void wait_for(tree_uint4 (&q)[N]) {
     for (int j = 0; j < N; ++j) asm volatile("" : "+v"(q[j]));
 }
 
+// What the lane's draft sees of the drafts: bits of the first 64 of them, requested ahead of the tiles (most trees have no more).
+__device__ __forceinline__ uint64_t first_drafts(const TreePlan& t, const Place& p, int draft) {
+    if (t.mask == nullptr) return draft >= 63 ? ~0ull : (2ull << draft) - 1;   // drafts 0 .. draft
+    return t.mask[((size_t)p.a * t.nodes + draft) * t.words];
+}
 // Bit t: draft `draft`'s rows see token t0 + t, among the tile's tokens `there`.
-__device__ __forceinline__ uint32_t seen_tokens(const TreePlan& t, const Place& p, int draft, int t0, uint32_t there) {
+__device__ __forceinline__ uint32_t seen_tokens(const TreePlan& t, const Place& p, int draft, uint64_t first, int t0, uint32_t there) {
     if (draft >= p.count) return 0;
     const int lead = t0 - p.before;   // the tile's first token as a draft
     if (lead + 32 <= 0) return there;
     uint32_t drafts;
-    if (t.mask == nullptr) {
-        const int n_seen = draft + 1 - lead;   // drafts 0 .. draft
-        drafts = n_seen >= 32 ? 0xFFFFFFFFu : n_seen > 0 ? (1u << n_seen) - 1 : 0u;
+    if (lead <= 0) {
+        drafts = (uint32_t)first << -lead | ((1u << -lead) - 1);   // with the tokens before the drafts
     } else {
-        const uint64_t* row_mask = t.mask + ((size_t)p.a * t.nodes + draft) * t.words;
-        if (lead >= 0) {
-            const int w = lead >> 6, by = lead & 63;
-            drafts = w < t.words ? (uint32_t)(row_mask[w] >> by) : 0u;
-            if (by > 32 && w + 1 < t.words) drafts |= (uint32_t)(row_mask[w + 1] << (64 - by));
-        } else {
-            drafts = (uint32_t)row_mask[0] << -lead;
-        }
+        const int w = lead >> 6, by = lead & 63;
+        auto word = [&](int i) -> uint64_t {
+            if (i == 0) return first;
+            if (t.mask == nullptr) return draft >= 64 * i + 63 ? ~0ull : draft >= 64 * i ? (2ull << (draft - 64 * i)) - 1 : 0ull;
+            return i < t.words ? t.mask[((size_t)p.a * t.nodes + draft) * t.words + i] : 0ull;
+        };
+        drafts = (uint32_t)(word(w) >> by);
+        if (by > 32) drafts |= (uint32_t)(word(w + 1) << (64 - by));
     }
-    if (lead < 0) drafts |= (1u << -lead) - 1;   // the tokens before the drafts
     return drafts & there;
 }
 
@@ -284,15 +287,38 @@ __device__ __forceinline__ size_t partial_row(const TreeArgs& g, const Place& p,
 
 constexpr float kRotation(int D) { return D == 64 ? 0.125f : D == 128 ? 0.08838834764831845f : 0.0625f; }
 
-// The pool's partials of a row: maximum and sum over its splits.
-__device__ __forceinline__ void pool_sums(const TreeArgs& g, size_t row, size_t stride, float* M, float* L) {
-    *M = -INFINITY, *L = 0.0f;
-    for (int s = 0; s < g.pool.nsplit; ++s) *M = fmaxf(*M, g.pool.ml[(row + s * stride) * 2]);
-    for (int s = 0; s < g.pool.nsplit; ++s) {
-        const float2 part = *reinterpret_cast<const float2*>(g.pool.ml + (row + s * stride) * 2);
-        *L = fmaf(part.y, __builtin_amdgcn_exp2f(part.x - *M), *L);   // (an empty split has m = -inf; the pool is not empty)
+// The pool's partials of a row: maxima and sums of its splits.  The first two are requested ahead of everything else (at head_dim
+// 256, whose registers are full, none are).
+template <int D> struct PoolSums {
+    static constexpr bool AHEAD = D != 256;
+    float m0, l0, m1, l1;
+
+    __device__ static __forceinline__ size_t row(const TreeArgs& g, const Place& p, int r, int s) {   // among the partials
+        return ((size_t)p.usel * g.pool.nsplit + s) * ((size_t)g.v.A * g.t.rows) + (size_t)p.a * g.t.rows + min(r, g.t.rows - 1);
     }
-}
+    __device__ __forceinline__ void request(const TreeArgs& g, const Place& p, int r) {
+        m0 = l0 = m1 = l1 = 0.0f;
+        if (AHEAD && g.pool.ml != nullptr && g.out != nullptr) {
+            const float2 a = load(g, p, r, 0), b = load(g, p, r, min(1, g.pool.nsplit - 1));
+            m0 = a.x, l0 = a.y, m1 = b.x, l1 = b.y;
+        }
+    }
+    __device__ static __forceinline__ float2 load(const TreeArgs& g, const Place& p, int r, int s) {
+        return *reinterpret_cast<const float2*>(g.pool.ml + row(g, p, r, s) * 2);
+    }
+    __device__ __forceinline__ float2 get(const TreeArgs& g, const Place& p, int r, int s) const {
+        if (!AHEAD || s > 1) return load(g, p, r, s);
+        return make_float2(s == 0 ? m0 : m1, s == 0 ? l0 : l1);
+    }
+    __device__ __forceinline__ void all(const TreeArgs& g, const Place& p, int r, float* M, float* L) const {
+        *M = -INFINITY, *L = 0.0f;
+        for (int s = 0; s < g.pool.nsplit; ++s) *M = fmaxf(*M, get(g, p, r, s).x);
+        for (int s = 0; s < g.pool.nsplit; ++s) {
+            const float2 x = get(g, p, r, s);
+            *L = fmaf(x.y, __builtin_amdgcn_exp2f(x.x - *M), *L);   // (an empty split has m = -inf; the pool is not empty)
+        }
+    }
+};
 
 // A wave's rows straight from the registers: partials, or, completed with the pool's, the output.
 // A lane has runs of consecutive coordinates of its row, the row's lanes in turn, so the inverse rotation of the pool's part is an
@@ -300,7 +326,7 @@ __device__ __forceinline__ void pool_sums(const TreeArgs& g, size_t row, size_t 
 //   permuted operands    block e has coordinates MG m + e: R / (4 LPR) runs of 4 MG, run k from MG (4 LPR k + 4 g)
 //   transposed operands  block e has coordinates R e + m: D / (4 LPR) runs of 4, run k from 4 LPR k + 4 g
 template <int D, bool BF, int R, bool TR>
-__device__ __forceinline__ void store_rows(const TreeArgs& g, const Place& p, const Rows<D, R>& x, int row0, int lane) {
+__device__ __forceinline__ void store_rows(const TreeArgs& g, const Place& p, const Rows<D, R>& x, const PoolSums<D>& pool, int row0, int lane) {
     constexpr int MG = D / R, LPR = 64 / R, C = TR ? 4 : 4 * MG, RUNS = D / (LPR * C), PER = R / (4 * LPR);   // PER: runs of a block
     const int h = lane / R, r = row0 + lane % R;
     auto first = [&](int k) { return C * (LPR * k + h); };
@@ -326,13 +352,12 @@ __device__ __forceinline__ void store_rows(const TreeArgs& g, const Place& p, co
     for (int i = 0; i < N; ++i) y[i] = 0.0f;
     float weight = 1.0f;
     if (g.pool.ml != nullptr) {
-        const size_t stride = (size_t)g.v.A * g.t.rows, row = (size_t)p.usel * g.pool.nsplit * stride + (size_t)p.a * g.t.rows + min(r, g.t.rows - 1);
         float M, L;
-        pool_sums(g, row, stride, &M, &L);
+        pool.all(g, p, r, &M, &L);
         const float top = fmaxf(M, m), scale = g.pool.rotated ? kRotation(D) : 1.0f;
         for (int s = 0; s < g.pool.nsplit; ++s) {
-            const float w = __builtin_amdgcn_exp2f(g.pool.ml[(row + s * stride) * 2] - top) * scale;
-            const float* src = g.pool.o + (row + s * stride) * D;
+            const float w = __builtin_amdgcn_exp2f(pool.get(g, p, r, s).x - top) * scale;
+            const float* src = g.pool.o + pool.row(g, p, r, s) * D;
 #pragma unroll
             for (int k = 0; k < RUNS; ++k)
 #pragma unroll
@@ -404,6 +429,8 @@ __global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D, R)) void at
     const Place pl = place_of(g);
     if (!pl.inside) return;
     const int row0 = pl.row_block * R;
+    PoolSums<D> pool;
+    pool.request(g, pl, row0 + (SHARE ? tid / (256 / R) : n));
     // the range's tiles; a block of rows that are all behind the agent's drafts sees none
     const int tiles = row0 < pl.count * t.G ? (pl.length + 31) >> 5 : 0;
     const int per_split = ((tiles + t.nsplit - 1) / t.nsplit + STEP - 1) & -STEP;
@@ -464,6 +491,7 @@ __global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D, R)) void at
         const int first_page = page_at(first);
         tree_uint4 q[KJ];
         const int draft = load_queries<D, R>(g, pl, row0, lane, q);
+        const uint64_t see_first = first_drafts(t, pl, draft);
         int row = row_at(first, first_page);
         load_keys(row);
         load_values(row);
@@ -513,7 +541,7 @@ __global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D, R)) void at
                         for (int w = 0; w < VW; ++w) x[u][w] = keep ? x[u][w] : 0;
                     }
                 }
-                const uint32_t seen = seen_tokens(t, pl, draft, t0, there);
+                const uint32_t seen = seen_tokens(t, pl, draft, see_first, t0, there);
                 if (seen & bad) poison = NAN;
                 hide_unseen<D, R>(s, seen, h);
             }
@@ -535,7 +563,7 @@ __global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D, R)) void at
         rows.l += poison;
     }
     if constexpr (!SHARE) {
-        store_rows<D, BF, R, false>(g, pl, rows, row0, lane);
+        store_rows<D, BF, R, false>(g, pl, rows, pool, row0, lane);
     } else {
         // ---- the waves' shares
         const float sum = row_sum<R>(rows.l);
@@ -559,9 +587,8 @@ __global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D, R)) void at
         for (int w = 1; w < 4; ++w) M = fmaxf(M, m_s[w][rr]);
         float L = 0.0f, pool_M = -INFINITY, pool_L = 0.0f;
         const bool last = g.out != nullptr, with_pool = last && g.pool.ml != nullptr;
-        const size_t stride = (size_t)v.A * t.rows, row = (size_t)pl.usel * g.pool.nsplit * stride + (size_t)pl.a * t.rows + min(r, t.rows - 1);
         if (with_pool) {
-            pool_sums(g, row, stride, &pool_M, &pool_L);
+            pool.all(g, pl, r, &pool_M, &pool_L);
             M = fmaxf(M, pool_M);
         }
         float f[4];
@@ -575,10 +602,10 @@ __global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D, R)) void at
         for (int i = 0; i < 4 * CG; ++i) y[i] = 0.0f;
         if (with_pool) {
             for (int s = 0; s < g.pool.nsplit; ++s) {
-                const float w = __builtin_amdgcn_exp2f(g.pool.ml[(row + s * stride) * 2] - M) * (g.pool.rotated ? kRotation(D) : 1.0f);
+                const float w = __builtin_amdgcn_exp2f(pool.get(g, pl, r, s).x - M) * (g.pool.rotated ? kRotation(D) : 1.0f);
 #pragma unroll
                 for (int c = 0; c < CG; ++c) {
-                    const float4 z = *reinterpret_cast<const float4*>(g.pool.o + (row + s * stride) * D + 4 * (TPR * c + part));
+                    const float4 z = *reinterpret_cast<const float4*>(g.pool.o + pool.row(g, pl, r, s) * D + 4 * (TPR * c + part));
                     float* d = y + 4 * c;
                     d[0] = fmaf(z.x, w, d[0]), d[1] = fmaf(z.y, w, d[1]), d[2] = fmaf(z.z, w, d[2]), d[3] = fmaf(z.w, w, d[3]);
                 }
@@ -653,6 +680,8 @@ __global__ __launch_bounds__(64 * W, many_waves_per_simd(D)) void attend_pages_m
     const int per_split = (tiles + t.nsplit - 1) / t.nsplit;
     const int t_begin = pl.split * per_split, t_end = min(tiles, t_begin + per_split);
     const int my_row0 = row0 + wave * kRows;
+    PoolSums<D> pool;
+    pool.request(g, pl, my_row0 + n);
 
     const size_t layer = (size_t)(t.layer_begin + pl.ls) * v.pages * v.H * v.P * D;
     const uint16_t* const Kb = v.K + layer;
@@ -713,6 +742,7 @@ __global__ __launch_bounds__(64 * W, many_waves_per_simd(D)) void attend_pages_m
         if constexpr (SETS > 2) ask(t_begin + 2, Set<2 % SETS>());
         tree_uint4 q[KJ];
         const int draft = load_queries<D, kRows>(g, pl, my_row0, lane, q);
+        const uint64_t see_first = first_drafts(t, pl, draft);
         float poison = 0.0f;
         if (draft >= pl.count) rows.m = 0.0f;   // such a row never sees a token: any reference will do
         stage(t_begin, Set<0>());
@@ -731,7 +761,7 @@ __global__ __launch_bounds__(64 * W, many_waves_per_simd(D)) void attend_pages_m
             const int flags = flag_s[tile & 1][n];
             const uint32_t there = (uint32_t)__ballot(flags & 1);
             if (there != 0xFFFFFFFFu || t0 + 32 > pl.before || my_row0 + kRows > pl.count * t.G) {
-                const uint32_t bad = (uint32_t)__ballot(flags & 2), seen = seen_tokens(t, pl, draft, t0, there);
+                const uint32_t bad = (uint32_t)__ballot(flags & 2), seen = seen_tokens(t, pl, draft, see_first, t0, there);
                 if (seen & bad) poison = NAN;
                 hide_unseen<D, kRows>(s, seen, h);
             }
@@ -762,7 +792,7 @@ __global__ __launch_bounds__(64 * W, many_waves_per_simd(D)) void attend_pages_m
         }
         rows.l += poison;
     }
-    store_rows<D, BF, kRows, true>(g, pl, rows, my_row0, lane);
+    store_rows<D, BF, kRows, true>(g, pl, rows, pool, my_row0, lane);
 }
 
 // -------------------------------------------------------------------------------------- merge ---
