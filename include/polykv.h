@@ -370,9 +370,9 @@ void polykv_codebook(float* centroids8, float* thresholds7);
 int polykv_codebook_bits(int bits, float* centroids, float* thresholds);
 
 /* Measurement hook (for benchmarks and profilers; not an operation of the method).  Arms the calling
- * thread: the NEXT pool_encode, pool_decode or pool_attend call of this thread that launches has the HIP runtime
+ * thread: the NEXT pool_encode, pool_decode, pool_attend or pool_attend_tree call of this thread that launches has the HIP runtime
  * record `start_event` when its main kernel (the encode kernel, the decode kernel, the pool attention
- * kernel -- not the tail and merge kernels; where polykv_attend_choice says tails_in_pool_launch, the private tails are
+ * kernel, without a pool the pages' -- not the tail and merge kernels; where polykv_attend_choice says tails_in_pool_launch, the private tails are
  * part of the pool kernel's launch and of the time) begins to execute and `stop_event` when it has finished,
  * on the stream the kernel is launched on; the hook then disarms itself.  Both are hipEvent_t handles
  * created (with timing enabled) and owned by the caller; either may be NULL.  hipEventElapsedTime(start,

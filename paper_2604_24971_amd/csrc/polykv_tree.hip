@@ -330,13 +330,15 @@ __device__ __forceinline__ void store_rows(const TreeArgs& g, const Place& p, co
     constexpr int MG = D / R, LPR = 64 / R, C = TR ? 4 : 4 * MG, RUNS = D / (LPR * C), PER = R / (4 * LPR);   // PER: runs of a block
     const int h = lane / R, r = row0 + lane % R;
     auto first = [&](int k) { return C * (LPR * k + h); };
-    auto acc = [&](int k, int c) { return TR ? x.acc[k / PER][4 * (k % PER) + c] : x.acc[c % MG][4 * k + c / MG]; };
     float sum = row_sum<R>(x.l);
-    const float m = sum == 0.0f ? -INFINITY : x.m;   // the row has seen no token (else its sum is 1 at the least)
+    const bool any = sum != 0.0f;   // the row has seen a token (its sum is then about 1 at the least)
+    // (a row that has seen none may share its wave with rows that have seen values that are not finite)
+    auto acc = [&](int k, int c) { return any ? TR ? x.acc[k / PER][4 * (k % PER) + c] : x.acc[c % MG][4 * k + c / MG] : 0.0f; };
+    const float m = any ? x.m : -INFINITY;
     if (g.out == nullptr) {
         if (r >= g.t.rows) return;
         const size_t prow = partial_row(g, p, r);
-        if (sum != 0.0f) {   // (else nobody reads its sums)
+        if (any) {   // (else nobody reads its sums)
 #pragma unroll
             for (int k = 0; k < RUNS; ++k)
 #pragma unroll
@@ -567,7 +569,8 @@ __global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D, R)) void at
     } else {
         // ---- the waves' shares
         const float sum = row_sum<R>(rows.l);
-        if (h == 0) m_s[wave][n] = sum == 0.0f ? -INFINITY : rows.m, l_s[wave][n] = sum;   // (no token: sum 0; else 1 at the least)
+        const bool any = sum != 0.0f;   // (as in store_rows)
+        if (h == 0) m_s[wave][n] = any ? rows.m : -INFINITY, l_s[wave][n] = sum;
         float* dst = o_s + (wave * R + n) * OSTRIDE;
 #pragma unroll
         for (int q = 0; q < S::AN / 4; ++q)
@@ -575,7 +578,7 @@ __global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D, R)) void at
             for (int c = 0; c < 4 * MG; c += 4) {
                 float y[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] = rows.acc[(c + i) % MG][4 * q + (c + i) / MG];
+                for (int i = 0; i < 4; ++i) y[i] = any ? rows.acc[(c + i) % MG][4 * q + (c + i) / MG] : 0.0f;
                 *reinterpret_cast<float4*>(dst + 4 * MG * (S::LPR * q + h) + c) = make_float4(y[0], y[1], y[2], y[3]);
             }
         __syncthreads();

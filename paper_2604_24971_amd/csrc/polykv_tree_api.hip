@@ -108,7 +108,7 @@ static int make_tree_plan(const polykv_pool* pool, const polykv_pages* pages, co
     t.qscale = plan->qscale;
     plan_tree(page_view(pages), prm->page_splits, &t);
     const int64_t units = (int64_t)t.layers * pages->kv_heads;
-    if ((units * pages->agents * t.nsplit + 8) * t.row_blocks > 0x7FFFFFFF) {
+    if ((units * pages->agents * t.nsplit + 8) * t.row_blocks > 0x7F000000) {   // (the grid is rounded up by less than 2^23)
         set_error("%s: %lld KV heads x %d agents x %d row blocks x %d splits are more workgroups than supported", who, (long long)units,
                   pages->agents, t.row_blocks, t.nsplit);
         return POLYKV_ESHAPE;
@@ -148,10 +148,13 @@ int polykv_pages_resize(const polykv_pages* pages, const int32_t* targets_dev, i
         set_error("%s: slots=%d outside [0, 2^30]", who, slots);
         return POLYKV_ESHAPE;
     }
-    if (targets_dev == pages->lengths_dev) {
-        set_error("%s: targets_dev must not be lengths_dev", who);
-        return POLYKV_EINVAL;
-    }
+    const void* own[] = {pages->table_dev, pages->lengths_dev, pages->free_dev, pages->free_state_dev, pages->ticket_dev};
+    for (const void* p : own)
+        if (p == targets_dev || p == slots_dev || p == offsets_dev || (slots_dev != nullptr && slots_dev == offsets_dev) ||
+            targets_dev == slots_dev || targets_dev == offsets_dev) {
+            set_error("%s: targets, slots and offsets must be arrays of their own", who);
+            return POLYKV_EINVAL;
+        }
     return hip_result(launch_pages_resize(pages, targets_dev, slots_dev, slots, offsets_dev, (hipStream_t)stream), who);
 }
 
@@ -200,6 +203,13 @@ int polykv_tree_masks(const int32_t* parents_dev, const int32_t* counts_dev, int
         set_error("%s: parents and mask must be device pointers, all arrays aligned to their elements", who);
         return POLYKV_EINVAL;
     }
+    const void *in[] = {parents_dev, counts_dev}, *out[] = {mask_dev, depth_dev};
+    for (const void* p : in)
+        for (const void* q : out)
+            if ((p != nullptr && p == q) || (const void*)mask_dev == (const void*)depth_dev) {
+                set_error("%s: an output must not be an input", who);
+                return POLYKV_EINVAL;
+            }
     return hip_result(launch_tree_masks(parents_dev, counts_dev, agents, nodes, mask_dev, depth_dev, (hipStream_t)stream), who);
 }
 

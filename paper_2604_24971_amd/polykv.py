@@ -116,6 +116,9 @@ def _load():
     lib.polykv_tree_masks.restype = ip
     lib.pool_attend_tree_workspace.argtypes = [vp, pp, tp]
     lib.pool_attend_tree_workspace.restype = sz
+    # The call enqueues several kernels that share a workspace.  It keeps the interpreter's lock, so that those of two threads
+    # on one stream do not mix (it takes a few microseconds and waits for nothing).
+    lib.pool_attend_tree = C.PyDLL(LIB_PATH).pool_attend_tree
     lib.pool_attend_tree.argtypes = [vp, pp, vp, vp, tp, vp]
     lib.pool_attend_tree.restype = ip
     lib.polykv_pages_accept.argtypes = [pp, vp, vp, vp, vp, ip, vp, vp, vp, vp, vp]
@@ -474,6 +477,8 @@ class Pages:
         self.layers, self.kv_heads, self.head_dim = layers, kv_heads, head_dim
         self.pages, self.page_tokens, self.agents, self.max_blocks, self.dtype = pages, page_tokens, agents, max_blocks, dtype
         device = torch.device(device)
+        if device.type != "cuda":
+            raise TypeError("pages lie in GPU memory, not on %s" % device)
         self.device = torch.device(device.type, device.index if device.index is not None else 0)
         shape = (layers, pages, kv_heads, page_tokens, head_dim)
         self.K = torch.empty(shape, dtype=dtype, device=self.device)
@@ -487,6 +492,8 @@ class Pages:
                                *(t.data_ptr() for t in (self.K, self.V, self.table, self.lengths, self.free, self.free_state,
                                                          self._ticket)))
         self._ref = C.byref(self._desc)
+        # (writing nothing checks the description)
+        _check(lib.polykv_pages_write(self._ref, None, None, _DTYPES[dtype], 0, 0, 0, 0, None, 0, layers, None))
         self._index = self.device.index
         self._per_agent, self._per_offset = self.lengths.shape, torch.Size((agents + 1,))
         self._workspaces = {}   # stream handle -> cached attend_tree workspace
@@ -523,8 +530,9 @@ class Pages:
             raise ValueError("K and V must be [%d, tokens, %d, %d]" % (layer_end - layer_begin, self.kv_heads, self.head_dim))
         if (dtype is not self.dtype and dtype is not torch.float32) or V.dtype is not dtype or K.device != device or V.device != device:
             raise TypeError("K and V must be %s or float32 tensors on %s" % (self.dtype, device))
-        strides = K.stride()
-        if strides[3] != 1 or V.stride() != strides:
+        # (what the stride of a dimension of one element is does not matter)
+        strides = [s if n > 1 else 0 for s, n in zip(K.stride(), shape)]
+        if strides[3] != 1 or [s if n > 1 else 0 for s, n in zip(V.stride(), shape)] != strides:
             raise ValueError("K and V must have the same strides, 1 along head_dim")
         _check(lib.polykv_pages_write(self._ref, K.data_ptr(), V.data_ptr(), _DTYPES[dtype], shape[1], strides[0], strides[1],
                                       strides[2], _ints(slots, (shape[1],), device, "slots"), layer_begin, layer_end,

@@ -143,6 +143,34 @@ def test_rising_and_far_apart_scores(d, dtype):
         s.check(s.pages.attend_tree(dev(Q, dtype), page_splits=splits), Q, [3, 3], None)
 
 
+@pytest.mark.parametrize("d,nodes,group,dtype", [(64, 8, 2, F16), (64, 30, 1, BF16), (64, 20, 3, F16), (64, 100, 1, BF16), (128, 4, 4, BF16),
+                                                 (128, 8, 4, F16), (128, 16, 4, BF16), (128, 32, 4, F16), (256, 8, 2, F16), (256, 24, 2, BF16)])
+def test_rising_scores_in_calls_of_many_heads(d, nodes, group, dtype):
+    """The same for the forms with rows of their own; scores of many thousands, where a product's rounding matters, among them."""
+    pk = _pk()
+    rng = np.random.default_rng(d + nodes)
+    s = Setup(rng, [nodes + 300, nodes + 77], d, dtype=dtype)
+    for a, n in enumerate(s.lengths):
+        for t in range(n):
+            s.K[:, s.table[a, t // 16], :, t % 16] *= t / 40.0
+    s.K = rounded(s.K, dtype)
+    s.load()
+    layers = 300
+    pages = pk.Pages(layers, 2, d, s.K.shape[1], 2, s.table.shape[1], dtype=dtype)
+    for name in ("K", "V"):
+        getattr(pages, name).copy_(getattr(s.pages, name).expand_as(pages.K))
+    pages.table.copy_(dev(s.table))
+    pages.lengths.copy_(s.pages.lengths)
+    for size in (1.0, -3.0, 0.01, 2e4):
+        Q1 = rounded(np.clip(rng.standard_normal((1, 2, nodes, 2 * group, d)) * size, -6e4, 6e4), dtype)     # (finite in fp16)
+        got = pages.attend_tree(dev(Q1, dtype).expand(layers, -1, -1, -1, -1).contiguous(), page_splits=1)
+        assert torch.equal(got, got[:1].expand_as(got))
+        if size < 1e3:
+            s.check(got[:1], Q1, [nodes, nodes], None)
+        else:   # (one token has all the weight, up to ties within the scores' rounding: the result is some mean of values)
+            assert torch.isfinite(got).all() and float(got.abs().max()) <= np.nanmax(np.abs(s.V)) * 1.01
+
+
 def test_queries_and_values_of_extreme_magnitude():
     rng = np.random.default_rng(11)
     for dtype, big in ((F16, 6e4), (BF16, 1e30)):
@@ -186,6 +214,153 @@ def test_what_a_draft_does_not_see_has_no_effect(d, dtype, bad):
         err = np.abs(clean.double().cpu().numpy() - out)[:, ~touched]
         tol = U.bound(out, mag, big, d, dtype, 70, 6.0)[:, ~touched]
         assert (err <= tol).all()
+
+
+@pytest.mark.parametrize("d,nodes,group", [(64, 2, 3), (128, 5, 4), (128, 20, 4), (256, 3, 4), (256, 40, 2)])
+def test_rows_without_drafts_beside_values_that_are_not_finite(d, nodes, group):
+    """An agent has fewer drafts than rows, and NaN and infinite vectors before them: its rows without a draft attend the pool
+    alone, without one they are 0, and other agents see nothing of it."""
+    rng = np.random.default_rng(d + nodes)
+    s = Setup(rng, [40, 100, 33], d, dtype=BF16)
+    broken = s.table[0, 1]
+    s.K[:, broken, :, 3], s.V[:, broken, :, 4:6] = np.nan, np.inf
+    s.load()
+    Q = rounded(rng.standard_normal((1, 3, nodes, 2 * group, d)), BF16)
+    pool, dense = _pool(rng, 1, 2, d, 64, BF16)
+    counts = np.array([1, nodes, 0], np.int32)
+    for splits in (1, 2):
+        for with_pool in (None, dense):
+            kw = dict(counts=dev(counts), page_splits=splits)
+            got = s.pages.attend_tree(dev(Q, BF16), **kw) if with_pool is None else pool.attend_tree(dev(Q, BF16), s.pages, **kw)
+            assert not torch.isfinite(got[0, 0, 0]).any()
+            got[0, 0, 0] = 0.0
+            lengths, s.lengths = s.lengths, np.array([0, 100, 33], np.int32)
+            Q0 = Q.copy()
+            got_rest, Q_rest = got[:, 1:], Q0[:, 1:]
+            out, mag, big = U.attend(Q_rest, s.K, s.V, s.table[1:], s.lengths[1:], counts[1:], None, with_pool)
+            tol = U.bound(out, mag, big, d, BF16, 164, 6.0, with_pool is not None)
+            assert (np.abs(got_rest.double().cpu().numpy() - out) <= tol).all()
+            alone = U.attend(Q[:, :1, 1:], s.K, s.V, s.table[:1], [0], [0], None, with_pool)
+            tol = U.bound(*alone, d, BF16, 164, 6.0, with_pool is not None)
+            assert (np.abs(got[:, :1, 1:].double().cpu().numpy() - alone[0]) <= tol).all()
+            s.lengths = lengths
+
+
+@pytest.mark.parametrize("d,nodes,group,dtype", [
+    (64, 5, 3, F16), (64, 16, 1, BF16), (64, 30, 1, F16), (64, 10, 3, BF16), (64, 20, 2, F16), (64, 33, 2, BF16), (64, 130, 1, F16),
+    (128, 4, 4, F16), (128, 3, 5, BF16), (128, 8, 4, BF16), (128, 25, 1, F16), (128, 13, 4, F16), (128, 41, 4, BF16), (128, 96, 1, F16),
+    (256, 8, 2, F16), (256, 16, 2, BF16), (256, 20, 5, F16)])
+@pytest.mark.parametrize("page_splits", [1, 2])
+def test_calls_of_many_heads(d, nodes, group, dtype, page_splits):
+    """Calls with many KV heads, where waves and workgroups have rows of their own: masks of any kind, agents with fewer drafts than
+    rows, drafts with values that are not finite, a page that is not there, NaN behind the tokens."""
+    pk = _pk()
+    rng = np.random.default_rng(7 * d + nodes + group)
+    lengths = [nodes, nodes + 1, nodes + 90, 0, nodes + 33, nodes + 130, max(nodes - 1, 1)]
+    A = len(lengths)
+    layers = 520 // (2 * A) + 1
+    s = Setup(rng, lengths, d, P=24, dtype=dtype)
+    s.table[5, 1] = -1
+    seen = rng.random((A, nodes, nodes)) < 0.5
+    seen[:, 1::5] = False
+    counts = np.array([nodes, max(nodes - 2, 0), nodes, nodes, nodes // 2, nodes, nodes], np.int32)
+    touched = np.zeros((A, nodes), bool)
+    for a in (0, 2, 4):      # a draft that some others see
+        if counts[a] < 2:
+            continue
+        i = int(counts[a]) // 2
+        t = lengths[a] - counts[a] + i
+        s.V[:, s.table[a, t // 24], :, t % 24, 1::2] = np.inf
+        touched[a, :counts[a]] = seen[a, :counts[a], i]
+    s.load()
+    pages = pk.Pages(layers, 2, d, s.K.shape[1], A, s.table.shape[1], page_tokens=24, dtype=dtype)
+    for name in ("K", "V"):
+        getattr(pages, name).copy_(getattr(s.pages, name).expand_as(pages.K))
+    pages.table.copy_(dev(s.table))
+    pages.lengths.copy_(s.pages.lengths)
+    Q1 = rounded(rng.standard_normal((1, A, nodes, 2 * group, d)), dtype)
+    Q = dev(Q1, dtype).expand(layers, -1, -1, -1, -1).contiguous()
+    got = pages.attend_tree(Q, counts=dev(counts), mask=dev(U.pack(seen)), page_splits=page_splits)
+    same = (got[:1].expand_as(got) == got) | got.isnan()
+    assert bool(same.all())
+    t = torch.from_numpy(touched).cuda()
+    assert not torch.isfinite(got[:, t]).any()
+    s.V[~np.isfinite(s.V)] = 0.0
+    clean = torch.where(t[None, :, :, None, None], 0.0, got[:1].float()).to(dtype)
+    out, mag, big = U.attend(Q1, s.K, s.V, s.table, s.lengths, counts, seen)
+    err = np.abs(clean.double().cpu().numpy() - out)[:, ~touched]
+    assert (err <= U.bound(out, mag, big, d, dtype, max(lengths), 6.0)[:, ~touched]).all()
+
+
+def _between_guards(nbytes):
+    """Memory with 4 KB of a pattern on both sides: (the whole, the part between)."""
+    raw = torch.full((4096 + (nbytes + 255) // 256 * 256 + 4096,), 0x5C, dtype=torch.uint8, device="cuda")
+    return raw, raw[4096:4096 + nbytes]
+
+
+def _untouched(raw, nbytes):
+    return bool((raw[:4096] == 0x5C).all()) and bool((raw[4096 + nbytes:] == 0x5C).all())
+
+
+@pytest.mark.parametrize("d,nodes,group,layers", [(64, 1, 1, 1), (64, 16, 1, 40), (64, 17, 1, 40), (64, 40, 1, 40), (64, 100, 1, 20), (128, 3, 5, 1),
+                                                  (128, 1, 5, 40), (128, 5, 5, 40), (128, 9, 5, 40), (128, 20, 5, 20), (256, 1, 3, 40), (256, 7, 3, 20),
+                                                  (256, 23, 3, 10)])
+def test_writes_stay_inside_the_output_and_the_workspace(d, nodes, group, layers):
+    """Every form of the kernel (few rows and many, shared and not), with and without splits and a pool."""
+    pk = _pk()
+    rng = np.random.default_rng(d + nodes)
+    lengths = [nodes, nodes + 70, 9, 150, 33, 64, 200, 31]
+    s = Setup(rng, lengths, d, L=1)
+    pages = pk.Pages(layers, 2, d, s.K.shape[1], len(lengths), s.table.shape[1], page_tokens=16)
+    pages.K.copy_(s.pages.K.expand_as(pages.K))
+    pages.V.copy_(s.pages.V.expand_as(pages.V))
+    pages.table.copy_(s.pages.table)
+    pages.lengths.copy_(s.pages.lengths)
+    pool, dense = _pool(rng, 1, 2, d, 70, F16)
+    big = pk.Pool(layers, 2, d, 70).bind()
+    K, V = pool.decode(F16)
+    big.encode(K.expand(layers, -1, -1, -1).contiguous(), V.expand(layers, -1, -1, -1).contiguous())
+    Kh, Vh = big.decode(torch.float32, layer_begin=0, layer_end=1)
+    dense = Kh.double().cpu().numpy(), Vh.double().cpu().numpy()
+    Q1 = rounded(rng.standard_normal((1, len(lengths), nodes, 2 * group, d)), F16)
+    Q = dev(Q1, F16).expand(layers, -1, -1, -1, -1).contiguous()
+    for p in (None, big):
+        for splits in (0, 1, 2):
+            need = pages.attend_tree_workspace_bytes(Q, p, page_splits=splits)
+            raw_w, ws = _between_guards(max(need, 256))
+            raw_o, out = _between_guards(Q.numel() * 2)
+            out = out.view(F16).view(Q.shape)
+            kw = dict(page_splits=splits, workspace=ws)
+            got = pages.attend_tree(Q, out, **kw) if p is None else p.attend_tree(Q, pages, out, **kw)
+            torch.cuda.synchronize()
+            assert _untouched(raw_w, max(need, 256)) and _untouched(raw_o, Q.numel() * 2)
+            assert torch.equal(got, got[:1].expand_as(got))
+            s.check(got[:1], Q1, np.full(len(lengths), nodes), None, pool=dense if p is not None else None)
+
+
+def test_two_threads_on_one_stream():
+    """Calls of different sizes from two threads, on the same stream and pages: each gets what it gets alone."""
+    import threading
+    rng = np.random.default_rng(6)
+    s = Setup(rng, [500, 300, 64], 128, L=2)
+    pool, _ = _pool(rng, 2, 2, 128, 700, F16)
+    Q = [dev(rng.standard_normal((2, 3, n, 8, 128)), F16) for n in (1, 7)]
+    want = [pool.attend_tree(q, s.pages, page_splits=3) for q in Q]
+    torch.cuda.synchronize()
+    got = [[], []]
+
+    def work(i):
+        for _ in range(40):
+            got[i].append(pool.attend_tree(Q[i], s.pages, page_splits=3))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(want[i], x) for x in got[i])
 
 
 def test_pages_that_are_not_there_and_lengths_out_of_range():
@@ -348,6 +523,9 @@ def test_write(d, H, P, dtype, src):
     pages.write(head_major[:, :, 0], head_major[:, :, 1], dev(slots))
     assert torch.equal(pages.K, wantK) and torch.equal(pages.V, wantV)
     pages.write(kv[:, :0, 0], kv[:, :0, 1], dev(slots[:0]))                     # nothing
+    single = kv[:, 7:8, 0].as_strided((L, 1, H, d), (kv.stride(0), 1, kv.stride(3), 1))     # a stride that nothing is read with
+    pages.write(single, kv[:, 7:8, 1], dev(np.array([5], np.int32)))
+    assert torch.equal(pages.K[:, 0, :, 5], kv[:, 7, 0].to(dtype)) and torch.equal(pages.V[:, 0, :, 5], kv[:, 7, 1].to(dtype))
     one = kv[:, 3:4, 0].expand(L, 2, H, d)                                       # one token for two slots
     pages.write(one, one, dev(np.array([4, 6], np.int32)))
     assert torch.equal(pages.K[:, 4 // P, :, 4 % P], kv[:, 3, 0].to(dtype)) and torch.equal(pages.V[:, 6 // P, :, 6 % P], kv[:, 3, 0].to(dtype))
@@ -533,6 +711,38 @@ def test_captured_steps_follow_the_lengths():
         for a, b in zip(eager, graphed):
             for x, y in zip(a.state(), b.state()):
                 assert torch.equal(x, y)
+
+
+def test_what_the_binding_refuses():
+    pk = _pk()
+    i32 = lambda *n: torch.zeros(n, dtype=torch.int32, device="cuda")  # noqa: E731
+    for bad in (dict(page_tokens=12), dict(agents=5000), dict(head_dim=96), dict(max_blocks=0)):
+        kw = dict(dict(layers=1, kv_heads=2, head_dim=64, pages=4, agents=3, max_blocks=2, page_tokens=8), **bad)
+        with pytest.raises(pk.PolyKVError):
+            pk.Pages(**kw)
+    with pytest.raises(TypeError):
+        pk.Pages(1, 2, 64, 4, 3, 2, device="cpu")
+    with pytest.raises(TypeError):
+        pk.Pages(1, 2, 64, 4, 3, 2, dtype=torch.float32)
+    p = pk.Pages(1, 2, 64, 4, 3, 2, page_tokens=8)
+    Q = torch.zeros((1, 3, 2, 4, 64), dtype=F16, device="cuda")
+    for call in (lambda: p.resize(i32(4)), lambda: p.resize(i32(3).long()), lambda: p.resize(i32(6)[::2]), lambda: p.resize(i32(3).cpu()),
+                 lambda: p.resize(i32(3), i32(5), i32(3)), lambda: p.attend_tree(Q.to(BF16)), lambda: p.attend_tree(Q, Q.float()),
+                 lambda: p.attend_tree(Q, counts=i32(2)), lambda: p.attend_tree(Q, mask=i32(3, 2, 1)),
+                 lambda: p.attend_tree(Q.transpose(2, 3).contiguous().transpose(2, 3)), lambda: pk.tree_masks(i32(3, 4).cpu()),
+                 lambda: pk.tree_masks(i32(3, 4), i32(4)), lambda: p.accept(i32(3, 4), i32(3, 5), i32(3, 4)),
+                 lambda: p.write(Q[:, 0, :, :2].float().half().to(BF16), Q[:, 0, :, :2].to(BF16), i32(2))):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: p.attend_tree(Q[:, :2]), lambda: p.attend_tree(Q[0]), lambda: p.attend_tree(Q, Q[:, :, :1]), lambda: p.accept(i32(2, 4), i32(2, 4), i32(2, 4)),
+                 lambda: p.attend_tree(Q, layer_begin=1), lambda: p.write(Q[:, 0], Q[:, 0], i32(2)),
+                 lambda: p.write(Q[:, 0, :, :2], Q[:, 0, :, :2].contiguous(), i32(2)), lambda: p.write(Q[:, 0, :, :2, ::2], Q[:, 0, :, :2, ::2], i32(2))):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(pk.PolyKVError):
+        p.attend_tree(torch.zeros((1, 3, 257, 4, 64), dtype=F16, device="cuda"))
+    with pytest.raises(pk.PolyKVError):
+        pk.Pool(1, 2, 64, 40).attend_tree(Q, p)          # nothing bound
 
 
 def test_on_another_stream_and_twice():

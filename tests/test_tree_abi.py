@@ -60,9 +60,12 @@ def test_resize_refusals():
     f = lib.polykv_pages_resize
     assert f(d, None, P, 10, P, None) == pk.EINVAL
     assert f(d, C.c_void_p(0x20000), P, 10, P, None) == pk.EINVAL          # the lengths themselves
-    assert f(d, C.c_void_p(0x10002), P, 10, P, None) == pk.EINVAL
-    assert f(d, P, P, -1, P, None) == pk.ESHAPE
-    assert f(d, P, P, 2 ** 30 + 1, P, None) == pk.ESHAPE
+    a, b, c = (C.c_void_p(0x40000 + 0x1000 * k) for k in range(3))
+    for args in ((a, P, 10, c), (a, b, 10, P), (P, b, 10, c), (a, a, 10, c), (a, b, 10, a), (a, b, 10, b), (a, C.c_void_p(0x20000), 10, c)):
+        assert f(d, *args, None) == pk.EINVAL                               # arrays that are also something else
+    assert f(d, C.c_void_p(0x10002), b, 10, c, None) == pk.EINVAL
+    assert f(d, a, b, -1, c, None) == pk.ESHAPE
+    assert f(d, a, b, 2 ** 30 + 1, c, None) == pk.ESHAPE
     assert f(C.byref(desc(free_dev=None)), P, P, 10, P, None) == pk.EINVAL
     assert f(C.byref(desc(free_state_dev=None)), P, P, 10, P, None) == pk.EINVAL
     assert f(C.byref(desc(ticket_dev=None)), P, P, 10, P, None) == pk.EINVAL
@@ -95,6 +98,9 @@ def test_masks_refusals():
     assert f(P, P, 0, 4, P, P, None) == pk.ESHAPE and f(P, P, 4097, 4, P, P, None) == pk.ESHAPE
     assert f(P, P, 3, 0, P, P, None) == pk.ESHAPE and f(P, P, 3, 257, P, P, None) == pk.ESHAPE
     assert f(P, P, 3, 4, C.c_void_p(0x10004), P, None) == pk.EINVAL
+    a, b = C.c_void_p(0x40000), C.c_void_p(0x50000)
+    for args in ((a, None, 3, 4, a, b), (a, None, 3, 4, b, a), (a, b, 3, 4, P, b), (a, b, 3, 4, b, P), (a, None, 3, 4, P, P)):
+        assert f(*args, None) == pk.EINVAL                                  # an output that is an input, or both outputs
 
 
 def test_accept_refusals():
