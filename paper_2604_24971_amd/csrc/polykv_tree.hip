@@ -659,30 +659,31 @@ __global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D, R)) void at
 // fetches for the tile after the next waits in registers until the tile before is done with.  (Keys straight from the pages as
 // operands, as above, are 32-byte pieces of 32 rows per load: four waves that fetch the same tile that way are bound by the L1.)
 template <int I> using Set = std::integral_constant<int, I>;
-constexpr int kRows = 32;   // rows of a wave
 constexpr int many_waves_per_simd(int D) { return D == 256 ? 1 : 2; }
 
 template <int D, bool BF, int W>
 __global__ __launch_bounds__(64 * W, many_waves_per_simd(D)) void attend_pages_many_kernel(TreeArgs g) {
-    constexpr int MG = D / 32, KJ = D / 16;
+    constexpr int R = 32;
+    using S = Shape<D, R>;
+    constexpr int MG = S::MG, KJ = S::KJ;
     constexpr int LPT = D / 8;                    // threads that fetch a token's row
     constexpr int TPP = 64 * W / LPT, NP = 32 / TPP;   // tokens of a pass, passes of a tile
     // Rows in LDS, in halves: 16 bytes more rotate the banks for the keys' operands (16 bytes of each of 32 rows), 64 bytes
-    // more for the values' (32 bytes of each of 4 rows).
+    // more for the values' (64 bytes of each of 4 rows).
     constexpr int KS = D + 8, VS = D + 32, TILE = 32 * (KS + VS);
     extern __shared__ __align__(16) uint16_t kv_s[];   // [2 tiles]([32][KS] keys, [32][VS] values)
     __shared__ int flag_s[2][32];                 // of a tile's token: 1 there, 2 a draft with a value that is not finite
     const PageView& v = g.v;
     const TreePlan& t = g.t;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int h = lane >> 5, n = lane & 31;
+    const int h = lane / R, n = lane % R;
     const Place pl = place_of(g);
     if (!pl.inside) return;
-    const int row0 = pl.row_block * kRows * W;
+    const int row0 = pl.row_block * R * W;
     const int tiles = row0 < pl.count * t.G ? (pl.length + 31) >> 5 : 0;
     const int per_split = (tiles + t.nsplit - 1) / t.nsplit;
     const int t_begin = pl.split * per_split, t_end = min(tiles, t_begin + per_split);
-    const int my_row0 = row0 + wave * kRows;
+    const int my_row0 = row0 + wave * R;
     PoolSums<D> pool;
     pool.request(g, pl, my_row0 + n);
 
@@ -731,7 +732,7 @@ __global__ __launch_bounds__(64 * W, many_waves_per_simd(D)) void attend_pages_m
         }
     };
 
-    Rows<D, kRows> rows;
+    Rows<D, R> rows;
     rows.clear();
     if (t_begin < t_end) {   // (the same for all waves)
         // Tile t_begin + i waits for LDS in register set i % SETS.
@@ -744,7 +745,7 @@ __global__ __launch_bounds__(64 * W, many_waves_per_simd(D)) void attend_pages_m
         if constexpr (SETS > 1) ask(t_begin + 1, Set<1 % SETS>());
         if constexpr (SETS > 2) ask(t_begin + 2, Set<2 % SETS>());
         tree_uint4 q[KJ];
-        const int draft = load_queries<D, kRows>(g, pl, my_row0, lane, q);
+        const int draft = load_queries<D, R>(g, pl, my_row0, lane, q);
         const uint64_t see_first = first_drafts(t, pl, draft);
         float poison = 0.0f;
         if (draft >= pl.count) rows.m = 0.0f;   // such a row never sees a token: any reference will do
@@ -756,29 +757,32 @@ __global__ __launch_bounds__(64 * W, many_waves_per_simd(D)) void attend_pages_m
         auto step = [&](int tile, auto next) {   // `next`: the set with the tile behind it
             uint16_t* const src = kv_s + (tile & 1) * TILE;
             const int t0 = 32 * tile;
-            Scores<kRows> s;
+            Scores<R> s;
             s.clear();
 #pragma unroll
             for (int j = 0; j < KJ; ++j)
-                s.t[0] = tree_mfma<BF, kRows>(*reinterpret_cast<const tree_uint4*>(src + n * KS + 16 * j + 8 * h), q[j], s.t[0]);
-            const int flags = flag_s[tile & 1][n];
+#pragma unroll
+                for (int u = 0; u < S::TT; ++u)
+                    s.t[u] = tree_mfma<BF, R>(*reinterpret_cast<const tree_uint4*>(src + (R * u + n) * KS + 8 * (S::LPR * j + h)), q[j], s.t[u]);
+            const int flags = flag_s[tile & 1][lane & 31];
             const uint32_t there = (uint32_t)__ballot(flags & 1);
-            if (there != 0xFFFFFFFFu || t0 + 32 > pl.before || my_row0 + kRows > pl.count * t.G) {
+            if (there != 0xFFFFFFFFu || t0 + 32 > pl.before || my_row0 + R > pl.count * t.G) {
                 const uint32_t bad = (uint32_t)__ballot(flags & 2), seen = seen_tokens(t, pl, draft, see_first, t0, there);
                 if (seen & bad) poison = NAN;
-                hide_unseen<D, kRows>(s, seen, h);
+                hide_unseen<D, R>(s, seen, h);
             }
-            const Weights<BF, kRows> w = weigh<D, BF, kRows>(rows, s, t.qscale);
+            const Weights<BF, R> w = weigh<D, BF, R>(rows, s, t.qscale);
             // values: sixteen lanes read 16 coordinates of four tokens and get four tokens of one coordinate each
-            uint16_t* const vals = src + 32 * KS + (4 * h + ((lane & 15) >> 2)) * VS + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+            uint16_t* const vals = src + 32 * KS + (4 * h + ((lane & 15) >> 2)) * VS + (n & 16) + 4 * (lane & 3);
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
+            for (int part = 0; part < S::PARTS; ++part)
 #pragma unroll
                 for (int e = 0; e < MG; ++e) {
-                    const uint2 lo = lds_transposed(vals + 16 * half * VS + 32 * e), hi = lds_transposed(vals + (16 * half + 8) * VS + 32 * e);
+                    uint16_t* const at = vals + S::token_of(8 * part) * VS + R * e;
+                    const uint2 lo = lds_transposed(at), hi = lds_transposed(at + S::token_of(4) * VS);
                     const tree_uint4 a = {lo.x, lo.y, hi.x, hi.y};
-                    rows.acc[e] = tree_mfma<BF, kRows>(a, w.p[half], rows.acc[e]);
-                    if constexpr (BF) rows.acc[e] = tree_mfma<BF, kRows>(a, w.low[half], rows.acc[e]);
+                    rows.acc[e] = tree_mfma<BF, R>(a, w.p[part], rows.acc[e]);
+                    if constexpr (BF) rows.acc[e] = tree_mfma<BF, R>(a, w.low[part], rows.acc[e]);
                 }
             if (tile + 1 < t_end) {
                 stage(tile + 1, next);
@@ -795,7 +799,7 @@ __global__ __launch_bounds__(64 * W, many_waves_per_simd(D)) void attend_pages_m
         }
         rows.l += poison;
     }
-    store_rows<D, BF, kRows, true>(g, pl, rows, pool, my_row0, lane);
+    store_rows<D, BF, R, true>(g, pl, rows, pool, my_row0, lane);
 }
 
 // -------------------------------------------------------------------------------------- merge ---
@@ -885,32 +889,38 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(AttendPlan p, int nspli
 }
 
 // ----------------------------------------------------------------------------------- launchers ---
+// Which form a call takes, by the rows of an agent and KV head and by how many agents and KV heads there are.  Measured, both sides:
+//   four waves share the rows where even so the waves do not fill the SIMDs twice: one layer of 15 agents x 64 rows over 112 tokens and a
+//     pool 37.4 us, 40.9 with a wave for 32 rows; all 24 layers of 100 agents with one row each 613 and 433 us;
+//   up to 16 rows a wave has 16: that last call 438 us with 32, 396;
+//     (at head_dim 256 32 rows do not fit a wave's registers beside keys and values on their way, and a wave always has 16);
+//   more than one wave's rows: two or four waves fetch the tiles together, four where two would not leave fewer waves idle: 128
+//     rows over 7,194 tokens 414 us, 514 with two; 160 rows over 300 tokens 261 us, 207 with two.
 void plan_tree(const PageView& v, int page_splits, TreePlan* t) {
-    const int row_tiles = (t->rows + kRows - 1) / kRows;
     const long tiles = ((long)v.max_blocks * v.P + 31) / 32, units = (long)t->layers * v.H * v.A;
+    const int row_tiles = (t->rows + 31) / 32;
     t->share = units * row_tiles <= 512 ? 1 : 0;
     t->wave_rows = t->rows <= 16 || v.D == 256 ? 16 : 32;
     t->waves = 1;
-    if (!t->share && (row_tiles > 1 || (v.D == 256 && t->rows > 16))) {
+    if (!t->share && t->rows > t->wave_rows) {
+        t->waves = (row_tiles + 3) / 4 * 4 <= (row_tiles + 1) / 2 * 2 ? 4 : 2;
         t->wave_rows = 32;
-        t->waves = 2;
-        if ((row_tiles + 3) / 4 * 4 <= (row_tiles + 1) / 2 * 2) t->waves = 4;
     }
     const int rows = t->wave_rows * t->waves;
     t->row_blocks = (t->rows + rows - 1) / rows;
     const long groups = units * t->row_blocks;
-    // Token ranges: the count with the least estimated time, in steps of a wave (one tile): rounds of workgroups over the places
-    // there are, times the steps of the longest continuation there can be plus four for the ramp and the final pass; more than
-    // one range adds the merge kernel and the partials.
-    const int wave_places = v.D == 256 ? 8 : t->wave_rows == 32 && t->waves == 1 ? (v.D == 64 ? 12 : 8) : t->waves > 1 ? 8 : v.D == 64 ? 16 : 12;
-    const int ways = t->share ? 4 : 1;
-    const long places = 256l * (wave_places / (t->share ? 4 : t->waves));
-    long want = 1, most = std::min((tiles + 3) / 4, 64l);
+    // Token ranges: the count with the least estimated time, in steps of a wave (one tile, about 1.5 us): rounds of workgroups over
+    // the places there are (waves that the registers leave room for), times the steps of the longest continuation there can be plus
+    // four for the ramp and the final pass; more than one range adds the merge kernel and its partials.
+    const int on_simd = t->waves > 1 ? many_waves_per_simd(v.D) : few_waves_per_simd(v.D, t->wave_rows), ways = t->share ? 4 : 1;
+    const long places = 256l * (4 * on_simd / (t->share ? 4 : t->waves));
+    const long most = std::min((tiles + 3) / 4, 64l);
     auto cost = [&](long n) {
         const double steps = (double)((tiles + n * ways - 1) / (n * ways)) + 4;
         const double rounds = (double)((groups * n + places - 1) / places);
         return rounds * steps + (n > 1 ? 6 + n * (double)units * t->rows * v.D * (8 / 4e12 / 1.5e-6) : 0.0);
     };
+    long want = 1;
     for (long n = 2; n <= most; ++n)
         if (cost(n) < cost(want)) want = n;
     if (page_splits > 0) want = std::min((long)page_splits, (tiles + 3) / 4);
