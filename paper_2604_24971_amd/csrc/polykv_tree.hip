@@ -803,21 +803,25 @@ __global__ __launch_bounds__(64 * W, many_waves_per_simd(D)) void attend_pages_m
 }
 
 // -------------------------------------------------------------------------------------- merge ---
-// One wave per row.  The pool's partials are added in the rotated domain and rotated back, the pages' join behind that.
-template <int D, bool BF>
-__global__ __launch_bounds__(256) void tree_merge_kernel(AttendPlan p, int nsplit, int page_nsplit, const float* __restrict__ pool_ml,
-                                                         const float* __restrict__ pool_o, const float* __restrict__ ml,
-                                                         const float* __restrict__ o, uint16_t* __restrict__ out) {
+// One wave per row, or (SHARE) eight that take every eighth partial each.  The pool's partials are added in the rotated domain and
+// rotated back, the pages' join behind that; what the eight waves have then is added through LDS.
+template <int D, bool BF, bool SHARE>
+__global__ __launch_bounds__(SHARE ? 512 : 256) void tree_merge_kernel(AttendPlan p, int nsplit, int page_nsplit, const float* __restrict__ pool_ml,
+                                                                       const float* __restrict__ pool_o, const float* __restrict__ ml,
+                                                                       const float* __restrict__ o, uint16_t* __restrict__ out) {
     constexpr int EPL = D / 64;
-    const int lane = threadIdx.x & 63;
-    const long row_global = ((long)blockIdx.y * gridDim.x + blockIdx.x) * 4 + (threadIdx.x >> 6), nrows = (long)p.layers * p.H * p.R;
+    constexpr int STEP = SHARE ? 8 : 1, B = SHARE ? 8 : 16;   // B partial rows are requested at once
+    __shared__ float2 x_s[SHARE ? 8 : 1][SHARE ? D / 2 : 1];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, turn = SHARE ? wave : 0;
+    const long block = (long)blockIdx.y * gridDim.x + blockIdx.x, row_global = SHARE ? block : block * 4 + wave;
+    const long nrows = (long)p.layers * p.H * p.R;
     const bool active = row_global < nrows;   // no early return: the butterflies need the whole wave
     const long rg = active ? row_global : 0;
     const int usel = (int)(rg / p.R), r = (int)(rg - (long)usel * p.R);
     int kvh;
     const int ls = p.div_H.divide(usel, &kvh);
     // Lane s holds (m, l) of split s: first the maximum over all splits, then sixty-four splits' weights at a time, which are handed
-    // out with readlane; eight partial rows are requested at once.
+    // out with readlane.
     auto sums_of = [&](const float* base, int n, int s) {
         return s < n ? *reinterpret_cast<const float2*>(base + (((size_t)usel * n + s) * p.R + r) * 2) : make_float2(-INFINITY, 0.0f);
     };
@@ -839,17 +843,18 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(AttendPlan p, int nspli
             L = fmaf(part.y, w, L);
             const int cnt = min(64, n - s0);
             const float* src = base_o + (((size_t)usel * n + s0) * p.R + r) * D + lane * EPL;
-            for (int k0 = 0; k0 < cnt; k0 += 8) {
-                float v[8][EPL], wk[8];
+            for (int k0 = turn; k0 < cnt; k0 += B * STEP) {
+                float v[B][EPL], wk[B];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    wk[k] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), min(k0 + k, 63)));
-                    const bool used = k0 + k < cnt && wk[k] != 0.0f;   // (sums that weigh nothing need not have been written)
+                for (int k = 0; k < B; ++k) {
+                    const int split = k0 + STEP * k;
+                    wk[k] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), min(split, 63)));
+                    const bool used = split < cnt && wk[k] != 0.0f;   // (sums that weigh nothing need not have been written)
 #pragma unroll
-                    for (int i = 0; i < EPL; ++i) v[k][i] = used ? src[(size_t)(k0 + k) * p.R * D + i] : 0.0f;
+                    for (int i = 0; i < EPL; ++i) v[k][i] = used ? src[(size_t)split * p.R * D + i] : 0.0f;
                 }
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
+                for (int k = 0; k < B; ++k)
 #pragma unroll
                     for (int i = 0; i < EPL; ++i) x[i] = fmaf(v[k][i], wk[k], x[i]);
             }
@@ -866,7 +871,7 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(AttendPlan p, int nspli
             x[i] = wht_lane_stage<8>(x[i], lane);
             x[i] = wht_lane_stage<16>(x[i], lane);
             x[i] = wht_lane_stage<32>(x[i], lane);
-            x[i] *= (D == 64 ? 0.125f : D == 128 ? 0.08838834764831845f : 0.0625f);
+            x[i] *= kRotation(D);
         }
         if (p.signs.on) flip_signs<EPL>(x, sign_word(p.signs, (lane * EPL) >> 5) >> ((lane * EPL) & 31));
     }
@@ -877,13 +882,23 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(AttendPlan p, int nspli
     L += lane_xor<8>(L);
     L = row_sum<16>(L);
     const float inv = L != 0.0f ? 1.0f / L : 0.0f;
-    if (active) {
-        uint16_t* dst = out + q_row_index(p, ls, kvh, r) * D + lane * EPL;
+    uint16_t* const dst = out + q_row_index(p, ls, kvh, r) * D;
+    if constexpr (SHARE) {   // (every workgroup has a row)
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) reinterpret_cast<float*>(x_s[wave])[lane * EPL + i] = x[i];
+        __syncthreads();
+        if (threadIdx.x < D / 2) {
+            float2 y = x_s[0][threadIdx.x];
+#pragma unroll
+            for (int w = 1; w < 8; ++w) y.x += x_s[w][threadIdx.x].x, y.y += x_s[w][threadIdx.x].y;
+            reinterpret_cast<uint32_t*>(dst)[threadIdx.x] = pack2<BF>(y.x * inv, y.y * inv);
+        }
+    } else if (active) {
         if constexpr (EPL == 1) {
-            *dst = (uint16_t)pack2<BF>(x[0] * inv, 0.0f);
+            dst[lane] = (uint16_t)pack2<BF>(x[0] * inv, 0.0f);
         } else {
 #pragma unroll
-            for (int i = 0; i < EPL; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = pack2<BF>(x[i] * inv, x[i + 1] * inv);
+            for (int i = 0; i < EPL; i += 2) *reinterpret_cast<uint32_t*>(dst + lane * EPL + i) = pack2<BF>(x[i] * inv, x[i + 1] * inv);
         }
     }
 }
@@ -968,15 +983,23 @@ hipError_t launch_attend_pages(const PageView& v, const TreePlan& t, bool bf16, 
     return hipGetLastError();
 }
 
+using MergeKernel = void (*)(AttendPlan, int, int, const float*, const float*, const float*, const float*, uint16_t*);
+template <int D> static MergeKernel merge_form(bool bf16, bool share) {
+    if (share) return bf16 ? tree_merge_kernel<D, true, true> : tree_merge_kernel<D, false, true>;
+    return bf16 ? tree_merge_kernel<D, true, false> : tree_merge_kernel<D, false, false>;
+}
+
+// Measured, fastest of ten, eight waves a row and one: 32 rows of head_dim 256 and 75 partials 7.6 and 21.3 us, 256 rows of 128
+// and 44 partials 5.1 and 6.7, 2,048 rows and 24 partials 14.7 and 6.5.
+constexpr long kMergeShareRows = 512;
+
 hipError_t launch_tree_merge(const AttendPlan& plan, const TreePlan& t, bool has_pool, const float* pool_ml, const float* pool_o,
                              const float* ml, const float* o, void* out, hipStream_t s) {
     const long nrows = (long)plan.layers * plan.H * plan.R;
-    using Kern = decltype(&tree_merge_kernel<64, false>);
-    static const Kern table[3][2] = {{tree_merge_kernel<64, false>, tree_merge_kernel<64, true>},
-                                     {tree_merge_kernel<128, false>, tree_merge_kernel<128, true>},
-                                     {tree_merge_kernel<256, false>, tree_merge_kernel<256, true>}};
-    launch_kernel(table[plan.D == 64 ? 0 : plan.D == 128 ? 1 : 2][plan.io_bf16 ? 1 : 0], grid_of((uint64_t)(nrows + 3) / 4), dim3(256), 0, s, {},
-                  plan, has_pool ? plan.nsplit : 0, t.nsplit, pool_ml, pool_o, ml, o, (uint16_t*)out);
+    const bool share = nrows <= kMergeShareRows;
+    launch_kernel(plan.D == 64 ? merge_form<64>(plan.io_bf16, share) : plan.D == 128 ? merge_form<128>(plan.io_bf16, share) : merge_form<256>(plan.io_bf16, share),
+                  grid_of(share ? (uint64_t)nrows : (uint64_t)(nrows + 3) / 4), dim3(share ? 512 : 256), 0, s, {}, plan, has_pool ? plan.nsplit : 0, t.nsplit,
+                  pool_ml, pool_o, ml, o, (uint16_t*)out);
     return hipGetLastError();
 }
 

@@ -113,6 +113,21 @@ def test_every_kind_of_pool(d, dtype, kw):
         s.check(pool.attend_tree(dev(Q, dtype), s.pages, mask=dev(U.pack(seen)), splits=splits), Q, [4, 4, 4], seen, pool=dense)
 
 
+@pytest.mark.parametrize("d,nodes,dtype", [(64, 3, BF16), (64, 130, F16), (128, 1, F16), (128, 90, BF16), (256, 2, BF16), (256, 87, F16)])
+def test_more_partials_than_a_wave_has_lanes(d, nodes, dtype):
+    """Calls of few and of many rows whose token ranges, 71 of the pages and up to 96 of the pool, are joined; most hold nothing of
+    the shorter agents, and one agent has no token at all."""
+    rng = np.random.default_rng(d + nodes)
+    s = Setup(rng, [9000, 140, 0], d, H=1, dtype=dtype)
+    Q = rounded(rng.standard_normal((1, 3, nodes, 2, d)), dtype)
+    counts = np.array([nodes, nodes // 2, 0], np.int32)
+    s.check(s.pages.attend_tree(dev(Q, dtype), counts=dev(counts), page_splits=71), Q, counts, None)
+    pool, dense = _pool(rng, 1, 1, d, 3100, dtype)
+    for page_splits in (2, 71):
+        got = pool.attend_tree(dev(Q, dtype), s.pages, counts=dev(counts), splits=96, page_splits=page_splits)
+        s.check(got, Q, counts, None, pool=dense)
+
+
 @pytest.mark.parametrize("dtype", [F16, BF16])
 def test_many_rows_and_the_largest_trees(dtype):
     rng = np.random.default_rng(5)
