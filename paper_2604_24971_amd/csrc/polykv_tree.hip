@@ -416,6 +416,10 @@ __device__ __forceinline__ void store_rows(const TreeArgs& g, const Place& p, co
 // keys when the scores of the tile before are done, its values when that tile's value products are.  A lane loads MG coordinates
 // of the tokens that its scores belong to and makes operands (eight tokens of one coordinate) of them by byte permutes.
 // SHARE: the four waves of a workgroup take every fourth tile and are joined through LDS; otherwise a workgroup is one wave.
+// Bound by memory where there are many agents and heads: 24 layers x 32 heads x 100 agents, one row over 61 to 121 tokens each (head_dim
+// 64), 1.84 GB in 312 us, 5.9 TB/s; 32 layers x 8 heads x 15 agents, 32 rows over 210 to 308 tokens (bfloat16, head_dim 128), 0.64 GB with
+// the pool's partials in 129 us, 4.9 TB/s.  By a wave's chain (queries, page, keys, two products, final pass) where there are few: one layer of
+// 15 agents 9.2 us.
 constexpr int few_waves_per_simd(int D, int R) { return R == 16 ? (D == 64 ? 4 : D == 128 ? 3 : 2) : D == 64 ? 3 : 2; }
 
 template <int D, bool BF, int R, bool SHARE>
@@ -658,6 +662,9 @@ __global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D, R)) void at
 // at a time, by all of them, and handed out through LDS, two tiles deep.  A thread fetches pieces of 16 bytes of a few tokens; what it
 // fetches for the tile after the next waits in registers until the tile before is done with.  (Keys straight from the pages as
 // operands, as above, are 32-byte pieces of 32 rows per load: four waves that fetch the same tile that way are bound by the L1.)
+// 128 rows over 7,194 tokens of 16 agents (4 layers x 8 heads, head_dim 128, 1.9 GB, 0.24 Tflop): 383 us at the fastest, where the loads
+// alone take 319 and the arithmetic alone 344.  Two waves a SIMD do not hide all of either behind the other; 64 rows a wave would halve
+// the LDS reads, but put a wave's sums into accumulation registers (521 us).
 template <int I> using Set = std::integral_constant<int, I>;
 constexpr int many_waves_per_simd(int D) { return D == 256 ? 1 : 2; }
 
