@@ -426,12 +426,18 @@ template <int D, bool BF, int R, bool SHARE>
 __global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D, R)) void attend_pages_few_kernel(TreeArgs g) {
     using S = Shape<D, R>;
     constexpr int MG = S::MG, KJ = S::KJ, SN = S::SN, VW = MG / 2, OSTRIDE = D + 4, STEP = SHARE ? 4 : 1;
+    // Head_dim 256: a tile's keys and values and the sums leave no registers for the queries, which wait in LDS (8 layers x 8 heads x 50
+    // agents over 300 tokens 143 us, 161 with them in registers and 60 bytes a lane of addresses in scratch).
+    constexpr bool Q_LDS = D == 256;
+    __shared__ tree_uint4 q_own[Q_LDS && !SHARE ? KJ * 64 : 1];
     extern __shared__ __align__(16) float o_s[];   // [4][R][OSTRIDE] (SHARE)
     __shared__ float m_s[SHARE ? 4 : 1][R], l_s[SHARE ? 4 : 1][R];
     const PageView& v = g.v;
     const TreePlan& t = g.t;
     const int tid = threadIdx.x, lane = tid & 63, wave = SHARE ? __builtin_amdgcn_readfirstlane(tid >> 6) : 0;
     const int h = lane / R, n = lane % R;
+    // (with SHARE where the wave's sums will be)
+    tree_uint4* const q_s = (SHARE ? reinterpret_cast<tree_uint4*>(o_s + wave * R * OSTRIDE) : q_own) + lane;
     const Place pl = place_of(g);
     if (!pl.inside) return;
     const int row0 = pl.row_block * R;
@@ -503,16 +509,24 @@ __global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D, R)) void at
         load_values(row);
         int page = first + STEP < t_end ? page_at(first + STEP) : -1;
         wait_for(q);
+        if constexpr (Q_LDS) {   // (each lane's own)
+#pragma unroll
+            for (int j = 0; j < KJ; ++j) q_s[64 * j] = q[j];
+        }
         float poison = 0.0f;
         if (draft >= pl.count) rows.m = 0.0f;   // such a row never sees a token: any reference will do
 
         for (int tile = first; tile < t_end; tile += STEP) {
             Scores<R> s;
             s.clear();
+            int at = 0;
+            if constexpr (Q_LDS) asm volatile("" : "+v"(at));   // (or they are read ahead of the loop)
 #pragma unroll
-            for (int j = 0; j < KJ; ++j)
+            for (int j = 0; j < KJ; ++j) {
+                const tree_uint4 qj = Q_LDS ? q_s[64 * j + at] : q[j];
 #pragma unroll
-                for (int u = 0; u < S::TT; ++u) s.t[u] = tree_mfma<BF, R>(k[u][j], q[j], s.t[u]);
+                for (int u = 0; u < S::TT; ++u) s.t[u] = tree_mfma<BF, R>(k[u][j], qj, s.t[u]);
+            }
             const int t0 = 32 * tile;
             const uint32_t there = (uint32_t)__ballot(row >= 0);   // (lanes 32 .. 63 repeat the tile's tokens)
             const bool more = tile + STEP < t_end;
@@ -567,6 +581,7 @@ __global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D, R)) void at
             row = next_row;
         }
         rows.l += poison;
+        if constexpr (Q_LDS) asm volatile("" ::: "memory");   // (the queries' place takes the sums)
     }
     if constexpr (!SHARE) {
         store_rows<D, BF, R, false>(g, pl, rows, pool, row0, lane);
