@@ -45,6 +45,7 @@ struct TreePlan {
     int layer_begin, layers, nodes, q_heads, G, rows;   // rows = nodes * G of an agent and KV head
     float qscale;
     int nsplit;                // token-range splits of the pages' part
+    int merge;                 // 1: the pages' kernel writes partials for the merge kernel, 0: the output
     int wave_rows;             // rows of a wave: 32, or 16 (waves == 1)
     int waves;                 // waves with rows of their own in a workgroup: 1 .. 4
     int share;                 // 1 (waves == 1): four waves share the rows
@@ -53,7 +54,7 @@ struct TreePlan {
     size_t off_ml, off_o, total;   // the pages' partials in the workspace (behind the pool's)
 };
 // Fills in the splits and the row blocks.
-void plan_tree(const PageView& v, int page_splits, TreePlan* t);
+void plan_tree(const PageView& v, int pool_splits, int page_splits, TreePlan* t);   // pool_splits: 0 without a pool
 // The pool's partials, to be joined with the pages': [units][nsplit][agents * rows].
 struct PoolPart {
     const float *ml, *o;   // nullptr: there is no pool

@@ -285,6 +285,11 @@ __device__ __forceinline__ size_t partial_row(const TreeArgs& g, const Place& p,
     return ((size_t)p.usel * g.t.nsplit + p.split) * ((size_t)g.v.A * g.t.rows) + (size_t)p.a * g.t.rows + r;
 }
 
+// Up to so many splits of the pool the pages' kernel joins itself; beyond it writes partials and the merge kernel joins all.  Measured,
+// joined here and by the merge kernel: one layer of 15 agents with a row each, 16 splits 18.3 and 19.7 us a call; of 4 agents with 4 x 4
+// rows, 16 splits, 18.5 and 20.1; of one agent with 70 rows, 42 splits, 29 and 18.
+constexpr int kJoinSplits = 16;
+
 constexpr float kRotation(int D) { return D == 64 ? 0.125f : D == 128 ? 0.08838834764831845f : 0.0625f; }
 
 // The pool's partials of a row: maxima and sums of its splits.  The first two are requested ahead of everything else (at head_dim
@@ -306,17 +311,58 @@ template <int D> struct PoolSums {
     __device__ static __forceinline__ float2 load(const TreeArgs& g, const Place& p, int r, int s) {
         return *reinterpret_cast<const float2*>(g.pool.ml + row(g, p, r, s) * 2);
     }
-    __device__ __forceinline__ float2 get(const TreeArgs& g, const Place& p, int r, int s) const {
-        if (!AHEAD || s > 1) return load(g, p, r, s);
-        return make_float2(s == 0 ? m0 : m1, s == 0 ? l0 : l1);
-    }
     __device__ __forceinline__ void all(const TreeArgs& g, const Place& p, int r, float* M, float* L) const {
         *M = -INFINITY, *L = 0.0f;
-        for (int s = 0; s < g.pool.nsplit; ++s) *M = fmaxf(*M, get(g, p, r, s).x);
-        for (int s = 0; s < g.pool.nsplit; ++s) {
-            const float2 x = get(g, p, r, s);
-            *L = fmaf(x.y, __builtin_amdgcn_exp2f(x.x - *M), *L);   // (an empty split has m = -inf; the pool is not empty)
+        auto take = [&](auto& x, float top) {
+            if (top == -INFINITY) return;   // (empty splits so far; the pool is not empty)
+            *L *= __builtin_amdgcn_exp2f(*M - top);
+            *M = top;
+#pragma unroll
+            for (const float2& y : x) *L = fmaf(y.y, __builtin_amdgcn_exp2f(y.x - top), *L);
+        };
+        if (AHEAD) {
+            const float2 x[2] = {make_float2(m0, l0), g.pool.nsplit > 1 ? make_float2(m1, l1) : make_float2(-INFINITY, 0.0f)};
+            take(x, fmaxf(x[0].x, x[1].x));
         }
+        constexpr int B = AHEAD ? 8 : 4;   // are requested before the first is used
+#pragma unroll 1
+        for (int s0 = AHEAD ? 2 : 0; s0 < g.pool.nsplit; s0 += B) {
+            float2 x[B];
+            float top = *M;
+#pragma unroll
+            for (int k = 0; k < B; ++k) x[k] = s0 + k < g.pool.nsplit ? load(g, p, r, s0 + k) : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+            for (int k = 0; k < B; ++k) top = fmaxf(top, x[k].x);
+            take(x, top);
+        }
+    }
+    // d += the value sums of a row's splits, each times 2^(m - M) * scale; coordinates base + at(i) .. + 3 in d[4 i] .. d[4 i + 3].
+    template <int N, class At> __device__ static __forceinline__ void add(const TreeArgs& g, const Place& p, int r, float M, float scale, float (&d)[N], At at) {
+        auto splits = [&](int s0, auto count) {   // all are requested before the first is used
+            constexpr int B = decltype(count)::value;
+            float4 z[B][N / 4];
+            float w[B];
+#pragma unroll
+            for (int k = 0; k < B; ++k) {
+                w[k] = load(g, p, r, s0 + k).x;
+                const float* src = g.pool.o + row(g, p, r, s0 + k) * D;
+#pragma unroll
+                for (int i = 0; i < N / 4; ++i) z[k][i] = *reinterpret_cast<const float4*>(src + at(i));
+            }
+#pragma unroll
+            for (int k = 0; k < B; ++k) {
+                const float f = __builtin_amdgcn_exp2f(w[k] - M) * scale;
+#pragma unroll
+                for (int i = 0; i < N / 4; ++i) {
+                    float* y = d + 4 * i;
+                    y[0] = fmaf(z[k][i].x, f, y[0]), y[1] = fmaf(z[k][i].y, f, y[1]), y[2] = fmaf(z[k][i].z, f, y[2]), y[3] = fmaf(z[k][i].w, f, y[3]);
+                }
+            }
+        };
+        int s0 = 0;
+        if constexpr (N < 64)   // (as far as the registers reach)
+            for (; s0 + 1 < g.pool.nsplit; s0 += 2) splits(s0, std::integral_constant<int, 2>());
+        for (; s0 < g.pool.nsplit; ++s0) splits(s0, std::integral_constant<int, 1>());
     }
 };
 
@@ -357,18 +403,7 @@ __device__ __forceinline__ void store_rows(const TreeArgs& g, const Place& p, co
         float M, L;
         pool.all(g, p, r, &M, &L);
         const float top = fmaxf(M, m), scale = g.pool.rotated ? kRotation(D) : 1.0f;
-        for (int s = 0; s < g.pool.nsplit; ++s) {
-            const float w = __builtin_amdgcn_exp2f(pool.get(g, p, r, s).x - top) * scale;
-            const float* src = g.pool.o + pool.row(g, p, r, s) * D;
-#pragma unroll
-            for (int k = 0; k < RUNS; ++k)
-#pragma unroll
-                for (int c = 0; c < C; c += 4) {
-                    const float4 z = *reinterpret_cast<const float4*>(src + first(k) + c);
-                    float* d = y + C * k + c;
-                    d[0] = fmaf(z.x, w, d[0]), d[1] = fmaf(z.y, w, d[1]), d[2] = fmaf(z.z, w, d[2]), d[3] = fmaf(z.w, w, d[3]);
-                }
-        }
+        pool.add(g, p, r, top, scale, y, [&](int i) { return first(4 * i / C) + 4 * i % C; });
         if (g.pool.rotated) {
             wht_inlane<N>(y);
 #pragma unroll
@@ -623,15 +658,7 @@ __global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D, R)) void at
 #pragma unroll
         for (int i = 0; i < 4 * CG; ++i) y[i] = 0.0f;
         if (with_pool) {
-            for (int s = 0; s < g.pool.nsplit; ++s) {
-                const float w = __builtin_amdgcn_exp2f(pool.get(g, pl, r, s).x - M) * (g.pool.rotated ? kRotation(D) : 1.0f);
-#pragma unroll
-                for (int c = 0; c < CG; ++c) {
-                    const float4 z = *reinterpret_cast<const float4*>(g.pool.o + pool.row(g, pl, r, s) * D + 4 * (TPR * c + part));
-                    float* d = y + 4 * c;
-                    d[0] = fmaf(z.x, w, d[0]), d[1] = fmaf(z.y, w, d[1]), d[2] = fmaf(z.z, w, d[2]), d[3] = fmaf(z.w, w, d[3]);
-                }
-            }
+            pool.add(g, pl, r, M, g.pool.rotated ? kRotation(D) : 1.0f, y, [&](int i) { return 4 * (TPR * i + part); });
             if (g.pool.rotated) {
                 wht_inlane<4 * CG>(y);
 #pragma unroll
@@ -933,7 +960,7 @@ __global__ __launch_bounds__(SHARE ? 512 : 256) void tree_merge_kernel(AttendPla
 //     (at head_dim 256 32 rows do not fit a wave's registers beside keys and values on their way, and a wave always has 16);
 //   more than one wave's rows: two or four waves fetch the tiles together, four where two would not leave fewer waves idle: 128
 //     rows over 7,194 tokens 414 us, 514 with two; 160 rows over 300 tokens 261 us, 207 with two.
-void plan_tree(const PageView& v, int page_splits, TreePlan* t) {
+void plan_tree(const PageView& v, int pool_splits, int page_splits, TreePlan* t) {
     const long tiles = ((long)v.max_blocks * v.P + 31) / 32, units = (long)t->layers * v.H * v.A;
     const int row_tiles = (t->rows + 31) / 32;
     t->share = units * row_tiles <= 512 ? 1 : 0;
@@ -955,13 +982,14 @@ void plan_tree(const PageView& v, int page_splits, TreePlan* t) {
     auto cost = [&](long n) {
         const double steps = (double)((tiles + n * ways - 1) / (n * ways)) + 4;
         const double rounds = (double)((groups * n + places - 1) / places);
-        return rounds * steps + (n > 1 ? 6 + n * (double)units * t->rows * v.D * (8 / 4e12 / 1.5e-6) : 0.0);
+        return rounds * steps + (n > 1 || pool_splits > kJoinSplits ? 6 + n * (double)units * t->rows * v.D * (8 / 4e12 / 1.5e-6) : 0.0);
     };
     long want = 1;
     for (long n = 2; n <= most; ++n)
         if (cost(n) < cost(want)) want = n;
     if (page_splits > 0) want = std::min((long)page_splits, (tiles + 3) / 4);
     t->nsplit = (int)want;
+    t->merge = want > 1 || pool_splits > kJoinSplits;
     t->div_H = FastDiv::by(v.H);
     t->div_A = FastDiv::by(v.A);
     t->div_G = FastDiv::by(t->G);

@@ -106,7 +106,7 @@ static int make_tree_plan(const polykv_pool* pool, const polykv_pages* pages, co
     t.layer_begin = plan->layer_begin, t.layers = plan->layers, t.nodes = prm->nodes, t.q_heads = plan->q_heads, t.G = plan->G;
     t.rows = prm->nodes * plan->G;
     t.qscale = plan->qscale;
-    plan_tree(page_view(pages), prm->page_splits, &t);
+    plan_tree(page_view(pages), pool != nullptr ? plan->nsplit : 0, prm->page_splits, &t);
     const int64_t units = (int64_t)t.layers * pages->kv_heads;
     if ((units * pages->agents * t.nsplit + 8) * t.row_blocks > 0x7F000000) {   // (the grid is rounded up by less than 2^23)
         set_error("%s: %lld KV heads x %d agents x %d row blocks x %d splits are more workgroups than supported", who, (long long)units,
@@ -115,7 +115,7 @@ static int make_tree_plan(const polykv_pool* pool, const polykv_pages* pages, co
     }
     size_t off = pool != nullptr ? plan->total : 0;
     t.off_ml = t.off_o = off;
-    if (t.nsplit > 1) {
+    if (t.merge) {
         off = align_up(off + (size_t)units * t.nsplit * plan->R * 2 * sizeof(float), 256);
         t.off_o = off;
         off = align_up(off + (size_t)units * t.nsplit * plan->R * plan->D * sizeof(float), 256);
@@ -259,10 +259,10 @@ int pool_attend_tree(const polykv_pool* pool, const polykv_pages* pages, const v
         part.rotated = plan.vcodec != POLYKV_VALUES_INT8;
         part.signs = plan.signs;
     }
-    // One token range per agent: the pages' kernel completes the rows.  Several: their partials, and the pool's, are joined after it.
-    hipError_t e = launch_attend_pages(page_view(pages), tree, pages->dtype == POLYKV_BF16, Q_dev, ml, o, tree.nsplit == 1 ? out_dev : nullptr,
+    // One token range per agent and few of the pool: the pages' kernel completes the rows.  Else the partials are joined after it.
+    hipError_t e = launch_attend_pages(page_view(pages), tree, pages->dtype == POLYKV_BF16, Q_dev, ml, o, tree.merge ? nullptr : out_dev,
                                        part, s);
-    if (e == hipSuccess && tree.nsplit > 1) e = launch_tree_merge(plan, tree, pool != nullptr, part.ml, part.o, ml, o, out_dev, s);
+    if (e == hipSuccess && tree.merge) e = launch_tree_merge(plan, tree, pool != nullptr, part.ml, part.o, ml, o, out_dev, s);
     return hip_result(e, who);
 }
 

@@ -353,6 +353,35 @@ def test_writes_stay_inside_the_output_and_the_workspace(d, nodes, group, layers
             s.check(got[:1], Q1, np.full(len(lengths), nodes), None, pool=dense if p is not None else None)
 
 
+@pytest.mark.parametrize("d,nodes,group,layers,dtype", [(64, 1, 1, 1, F16), (64, 16, 1, 40, BF16), (64, 17, 1, 40, F16), (64, 40, 1, 40, F16),
+                                                        (64, 100, 1, 20, BF16), (128, 3, 5, 1, BF16), (128, 5, 1, 40, BF16), (128, 5, 5, 40, F16),
+                                                        (128, 20, 5, 20, F16), (256, 1, 3, 1, F16), (256, 1, 3, 40, BF16), (256, 23, 3, 10, F16)])
+def test_joining_the_pools_splits(d, nodes, group, layers, dtype):
+    """Every form of the kernel with one token range of the pages and one, two, several and more splits of the pool than it joins
+    itself; the agents hold a few tokens, or none."""
+    pk = _pk()
+    rng = np.random.default_rng(d + nodes + 1)
+    lengths = [nodes, nodes + 40, 0, 33, nodes + 1, 5, 64, 2]
+    s = Setup(rng, lengths, d, L=1, dtype=dtype)
+    pages = pk.Pages(layers, 2, d, s.K.shape[1], len(lengths), s.table.shape[1], page_tokens=16, dtype=dtype)
+    pages.K.copy_(s.pages.K.expand_as(pages.K))
+    pages.V.copy_(s.pages.V.expand_as(pages.V))
+    pages.table.copy_(s.pages.table)
+    pages.lengths.copy_(s.pages.lengths)
+    K = dev(0.3 * rng.standard_normal((1, 2, 700, d)), dtype)
+    V = dev(rng.standard_normal((1, 2, 700, d)), dtype)
+    pool = pk.Pool(layers, 2, d, 700).bind()
+    pool.encode(K.expand(layers, -1, -1, -1).contiguous(), V.expand(layers, -1, -1, -1).contiguous())
+    Kh, Vh = pool.decode(torch.float32, layer_begin=0, layer_end=1)
+    dense = Kh.double().cpu().numpy(), Vh.double().cpu().numpy()
+    Q1 = rounded(rng.standard_normal((1, len(lengths), nodes, 2 * group, d)), dtype)
+    Q = dev(Q1, dtype).expand(layers, -1, -1, -1, -1).contiguous()
+    for splits in (1, 2, 3, 10, 16, 17):
+        got = pool.attend_tree(Q, pages, splits=splits, page_splits=1)
+        assert torch.equal(got, got[:1].expand_as(got))
+        s.check(got[:1], Q1, np.full(len(lengths), nodes), None, pool=dense)
+
+
 def test_two_threads_on_one_stream():
     """Calls of different sizes from two threads, on the same stream and pages: each gets what it gets alone."""
     import threading
