@@ -451,7 +451,7 @@ def tree_masks(parents: torch.Tensor, counts: torch.Tensor | None = None, mask: 
     elif mask.dtype is not torch.int64 or mask.shape != words or mask.device != device or not mask.is_contiguous():
         raise TypeError("mask must be a contiguous int64 tensor of shape %s on %s" % (words, device))
     if depth is None:
-        depth = _new(shape, torch.int32, device, stream)
+        depth = torch.empty_like(parents) if stream is None else _new(shape, torch.int32, device, stream)
     _check(lib.polykv_tree_masks(_ints(parents, shape, device, "parents"),
                                  _ints(counts, (agents,), device, "counts") if counts is not None else None, agents, nodes,
                                  mask.data_ptr(), _ints(depth, shape, device, "depth"), _stream_ptr(stream)))
@@ -530,13 +530,14 @@ class Pages:
             raise ValueError("K and V must be [%d, tokens, %d, %d]" % (layer_end - layer_begin, self.kv_heads, self.head_dim))
         if (dtype is not self.dtype and dtype is not torch.float32) or V.dtype is not dtype or K.device != device or V.device != device:
             raise TypeError("K and V must be %s or float32 tensors on %s" % (self.dtype, device))
-        # (what the stride of a dimension of one element is does not matter)
-        strides = [s if n > 1 else 0 for s, n in zip(K.stride(), shape)]
-        if strides[3] != 1 or [s if n > 1 else 0 for s, n in zip(V.stride(), shape)] != strides:
-            raise ValueError("K and V must have the same strides, 1 along head_dim")
-        _check(lib.polykv_pages_write(self._ref, K.data_ptr(), V.data_ptr(), _DTYPES[dtype], shape[1], strides[0], strides[1],
-                                      strides[2], _ints(slots, (shape[1],), device, "slots"), layer_begin, layer_end,
-                                      _stream_ptr(stream)))
+        strides = K.stride()
+        if strides != V.stride() or strides[3] != 1 or 1 in shape[1:]:   # (a dimension of one element: its stride does not matter)
+            strides = [s if n > 1 else 0 for s, n in zip(strides, shape)]
+            if strides[3] != 1 or [s if n > 1 else 0 for s, n in zip(V.stride(), shape)] != strides:
+                raise ValueError("K and V must have the same strides, 1 along head_dim")
+        _check(lib.polykv_pages_write(self._ref, K.data_ptr(), V.data_ptr(), _DTYPES[dtype], shape[1],
+                                      strides[0] if shape[0] > 1 else 0, strides[1], strides[2],
+                                      _ints(slots, (shape[1],), device, "slots"), layer_begin, layer_end, _stream_ptr(stream)))
 
     # pool_attend_tree(NULL, Q[drafts], out)
     def attend_tree(self, Q: torch.Tensor, out: torch.Tensor | None = None, **kw):
