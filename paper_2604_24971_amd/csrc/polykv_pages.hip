@@ -5,8 +5,6 @@
 #include <hip/hip_bf16.h>
 #include <hip/hip_fp16.h>
 
-#include <mutex>
-
 #include "polykv_pages.hpp"
 
 namespace polykv {
@@ -189,13 +187,10 @@ hipError_t launch_pages_resize(const polykv_pages* p, const int32_t* targets, in
                                hipStream_t s) {
     const PageView v = page_view(p);
     const int shared = 4 * v.A * (int)sizeof(int);
-    static std::once_flag configured;
-    static hipError_t config_result = hipSuccess;
-    std::call_once(configured, []() {
-        config_result = hipFuncSetAttribute(reinterpret_cast<const void*>(pages_resize_kernel<1024>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                            4 * POLYKV_MAX_PAGED_AGENTS * (int)sizeof(int));
-    });
-    if (config_result != hipSuccess) return config_result;
+    if (shared > 48 * 1024) {   // (by call: the attribute belongs to the current device)
+        const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(pages_resize_kernel<1024>), hipFuncAttributeMaxDynamicSharedMemorySize, shared);
+        if (err != hipSuccess) return err;
+    }
     if (slots == nullptr) n_slots = 0;
     if (v.A <= 64 && n_slots <= 4096) {
         launch_kernel(pages_resize_kernel<256>, dim3(1), dim3(256), shared, s, {}, v, targets, p->free_dev, p->free_state_dev, p->ticket_dev, slots,

@@ -8,7 +8,6 @@
 #include <hip/hip_fp16.h>
 
 #include <algorithm>
-#include <mutex>
 #include <type_traits>
 
 #include "polykv_layout.hpp"
