@@ -254,6 +254,12 @@ class Pool:
 
     __del__ = close
 
+    def _handle(self, what: str):
+        """For the calls whose pool may also be absent: a closed one is not an absent one."""
+        if self._h is None:
+            raise PolyKVError(EINVAL, "%s: the pool is closed" % what)
+        return self._h
+
     # pool_encode(K, V)
     def encode(self, K: torch.Tensor, V: torch.Tensor, stream=None):
         shape = (self.layers, self.kv_heads, self.tokens, self.head_dim)
@@ -407,9 +413,10 @@ class Pool:
                     key_precision=KEY_PRECISION_EXACT, **kw):
         """Attention of every agent's drafted tokens over this pool, then the agent's tokens in `pages` and the drafts
         among them that a draft sees; the further arguments are Pages.attend_tree()'s."""
+        handle = self._handle("attend_tree")
         if self.storage is not None and self.storage.device != pages.device:
             raise ValueError("the pool is on %s, the pages on %s" % (self.storage.device, pages.device))
-        return pages._attend_tree(self._h, Q, out, kernel=kernel, splits=splits, key_precision=key_precision, **kw)
+        return pages._attend_tree(handle, Q, out, kernel=kernel, splits=splits, key_precision=key_precision, **kw)
 
 
 # Calls act on the current device and on streams of it; an object on another device switches to it for the call.
@@ -603,8 +610,9 @@ class Pages:
     def attend_tree_workspace_bytes(self, Q, pool: "Pool | None" = None, *, layer_begin=0, layer_end=None, kernel=KERNEL_AUTO, splits=0,
                                     page_splits=0):
         """Scratch that attend_tree(Q) needs (with a pool: pool.attend_tree(Q, pages)); 0: none."""
+        handle = pool._handle("attend_tree_workspace_bytes") if pool is not None else None
         p = self._tree_params(Q, layer_begin, layer_end, None, kernel, splits, page_splits, KEY_PRECISION_EXACT)
-        return lib.pool_attend_tree_workspace(pool._h if pool is not None else None, self._ref, C.byref(p))
+        return lib.pool_attend_tree_workspace(handle, self._ref, C.byref(p))
 
     # polykv_pages_accept(tokens, following, parents)
     def accept(self, tokens: torch.Tensor, following: torch.Tensor, parents: torch.Tensor, counts: torch.Tensor | None = None,

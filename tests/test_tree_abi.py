@@ -157,3 +157,14 @@ def test_attend_refusals_and_sizes():
     assert f(None, d, P, P, C.byref(params(page_splits=4)), None) == pk.EINVAL
     assert f(None, d, P, P, C.byref(params(page_splits=4, workspace_dev=0x100080, workspace_bytes=need)), None) == pk.EINVAL
     assert f(None, d, P, P, C.byref(params(page_splits=4, workspace_dev=0x100000, workspace_bytes=need - 1)), None) == pk.ENOMEM
+
+
+def test_a_closed_pool_is_not_an_absent_one():
+    """The C calls take a pool of NULL for none; the binding does not hand a closed one on to them."""
+    pool = pk.Pool(2, 2, 64, 100)
+    pool.close()
+    pages = pk.Pages.__new__(pk.Pages)     # (its tensors would be on a GPU; no call gets as far as them)
+    for call in (lambda: pool.attend_tree(None, pages), lambda: pages.attend_tree_workspace_bytes(None, pool)):
+        with pytest.raises(pk.PolyKVError) as e:
+            call()
+        assert e.value.status == pk.EINVAL and "closed" in str(e.value)
