@@ -256,14 +256,16 @@ int pool_attend_static(const polykv_pool* pool, const void* Q_dev, void* out_dev
  * calls below keep the continuations of any number of agents in pages of a common store, with block tables and lengths
  * on the device (a captured graph sees them as they are when it is replayed), and serve steps in which every agent has
  * several drafted tokens that form a tree: a step is
- *   polykv_pages_resize   room for the drafts: block tables and the slots of the new tokens
+ *   polykv_pages_resize_by_agent   room for the drafts: block tables, the slots of the new tokens, and how many of them each
+ *                         agent has -- none where there was no room; these are the counts of the next four calls
  *   polykv_tree_masks     which drafts a draft sees, and its depth, from the tree's parents
  *   polykv_pages_write    the drafts' keys and values into their slots (layer by layer, or all layers)
  *   pool_attend_tree      attention of the drafts over the shared pool, the agent's own tokens and the drafts they see
  *   polykv_pages_accept   the path that the model agrees with; its keys and values move to where they stay
  *   polykv_pages_resize   back to the accepted lengths: pages that are no longer needed are free again
  * An agent's drafts are the last tokens of its continuation: with lengths[a] tokens in its pages and counts[a] drafts,
- * token lengths[a] - counts[a] + i is draft i.  A drafted token per agent (nodes = 1) is plain decoding.
+ * token lengths[a] - counts[a] + i is draft i.  A drafted token per agent (nodes = 1) is plain decoding.  An agent that did not grow
+ * by its drafts must have a count of 0: with any other its last tokens would be taken for drafts, and accept would cut them.
  *
  * The struct describes the caller's buffers and is read during a call only.  What lies in device memory cannot be
  * checked by the host: lengths outside [0, max_blocks * page_tokens] and counts outside [0, nodes] are taken as the
@@ -305,6 +307,13 @@ typedef struct {
  * offsets_dev (NULL: not wanted): int32 [agents + 1]. */
 int polykv_pages_resize(const polykv_pages* pages, const int32_t* targets_dev, int32_t* slots_dev, int slots,
                         int32_t* offsets_dev, void* stream);
+
+/* The same, for rows that have places by agent whoever grew: slots_dev (NULL: not wanted) is [agents, per_agent], entry (a, i) belongs to
+ * token (old length) + i of agent a, and entries from its growth on are -1 (tokens past per_agent have no entry); granted_dev
+ * (NULL: not wanted), int32 [agents], receives how many tokens each agent grew by, 0 if its target was no larger than its length,
+ * out of range, or asked for pages that are not there.  agents * per_agent <= 2^30. */
+int polykv_pages_resize_by_agent(const polykv_pages* pages, const int32_t* targets_dev, int32_t* slots_dev, int per_agent,
+                                 int32_t* granted_dev, void* stream);
 
 /* Keys and values of `tokens` tokens into the pages of layers [layer_begin, layer_end): vector (layer, token t, head) is
  * at element layer * layer_stride + t * token_stride + head * head_stride of K_dev / V_dev (the same strides for both)

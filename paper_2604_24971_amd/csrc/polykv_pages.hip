@@ -5,6 +5,8 @@
 #include <hip/hip_bf16.h>
 #include <hip/hip_fp16.h>
 
+#include <algorithm>
+
 #include "polykv_pages.hpp"
 
 namespace polykv {
@@ -56,10 +58,12 @@ __device__ __forceinline__ AgentChange change_of(const PageView& v, const int32_
 // A step of few agents is all latency: 256 threads there (15 agents that grow by 16 tokens each: 3.4 us at the fastest, with 1,024
 // threads 4.4).  1,024 agents that grow by up to 600 tokens take 9.3 us, and 6.1 to shrink: the four rounds of sums in front of
 // everything, then one round of stores.
-template <int THREADS>
+// BY_AGENT: the slot map has per_agent.d entries for every agent and the third output is how far each grew, for callers whose rows
+// have places by agent: an agent that got nothing then moves nobody else's slots.
+template <int THREADS, bool BY_AGENT>
 __global__ __launch_bounds__(THREADS) void pages_resize_kernel(PageView v, const int32_t* __restrict__ targets, int32_t* ring,
-                                                                      int32_t* state, int32_t* ticket, int32_t* __restrict__ slots, int n_slots,
-                                                                      int32_t* __restrict__ offsets) {
+                                                               int32_t* state, int32_t* ticket, int32_t* __restrict__ slots, int n_slots,
+                                                               int32_t* __restrict__ offsets, FastDiv per_agent) {
     extern __shared__ int shared[];
     int* const end_s = shared;                 // where an agent's new tokens end in the slot map
     int* const len_s = shared + v.A;           // its length
@@ -134,10 +138,18 @@ __global__ __launch_bounds__(THREADS) void pages_resize_kernel(PageView v, const
             row[b] = -1;
         }
     }
-    // four slots of a thread: one bisection, and then on from agent to agent
+    // page and place of an agent's new token t
+    auto page_of = [&](int a, int t, int* off) {
+        int rem;
+        int have = v.div_P.divide(len_s[a], &rem);
+        have += rem > 0;
+        const int b = v.div_P.divide(t, off);
+        return b < have ? v.table[(size_t)a * v.max_blocks + b] : ring[(first + (uint32_t)at_s[a] + (uint32_t)(b - have)) % NP];
+    };
+    // four slots of a thread
     for (int i0 = 4 * (blockIdx.x * THREADS + tid); i0 < n_slots; i0 += 4 * gridDim.x * THREADS) {
         int a = 0;
-        if (i0 < grown) {   // the first agent whose tokens end behind i0
+        if (!BY_AGENT && i0 < grown) {   // one bisection, and then on from agent to agent: the first whose tokens end behind i0
             int hi = v.A - 1;
             while (a < hi) {
                 const int mid = (a + hi) >> 1;
@@ -150,23 +162,29 @@ __global__ __launch_bounds__(THREADS) void pages_resize_kernel(PageView v, const
         for (int u = 0; u < 4; ++u) {
             page[u] = -1, off[u] = 0;
             const int i = i0 + u;
-            if (i >= grown) continue;
-            while (a < v.A - 1 && end_s[a] <= i) ++a;
-            int rem;
-            int have = v.div_P.divide(len_s[a], &rem);
-            have += rem > 0;
-            // (in range for whatever the sums hold)
-            const int t = min(max(tgt_s[a] - (end_s[a] - i), 0), v.max_blocks * v.P - 1);
-            const int b = v.div_P.divide(t, &off[u]);
-            page[u] = b < have ? v.table[(size_t)a * v.max_blocks + b] : ring[(first + (uint32_t)at_s[a] + (uint32_t)(b - have)) % NP];
+            if constexpr (BY_AGENT) {
+                if (i >= n_slots) continue;
+                int k;
+                a = per_agent.divide(i, &k);
+                if (k < tgt_s[a] - len_s[a]) page[u] = page_of(a, len_s[a] + k, &off[u]);
+            } else {
+                if (i >= grown) continue;
+                while (a < v.A - 1 && end_s[a] <= i) ++a;
+                // (in range for whatever the sums hold)
+                page[u] = page_of(a, min(max(tgt_s[a] - (end_s[a] - i), 0), v.max_blocks * v.P - 1), &off[u]);
+            }
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
             if (i0 + u < n_slots) slots[i0 + u] = (uint32_t)page[u] < NP ? page[u] * v.P + off[u] : -1;
     }
     if (offsets != nullptr && blockIdx.x == 0) {
-        for (int a = tid; a < v.A; a += THREADS) offsets[a + 1] = end_s[a];
-        if (tid == 0) offsets[0] = 0;
+        if constexpr (BY_AGENT) {
+            for (int a = tid; a < v.A; a += THREADS) offsets[a] = max(tgt_s[a] - len_s[a], 0);
+        } else {
+            for (int a = tid; a < v.A; a += THREADS) offsets[a + 1] = end_s[a];
+            if (tid == 0) offsets[0] = 0;
+        }
     }
     __shared__ int last_s;
     if (gridDim.x > 1) {   // (what this workgroup has read of lengths and state is in LDS and registers by now)
@@ -183,24 +201,35 @@ __global__ __launch_bounds__(THREADS) void pages_resize_kernel(PageView v, const
     }
 }
 
-hipError_t launch_pages_resize(const polykv_pages* p, const int32_t* targets, int32_t* slots, int n_slots, int32_t* offsets,
-                               hipStream_t s) {
+template <bool BY_AGENT>
+static hipError_t launch_resize(const polykv_pages* p, const int32_t* targets, int32_t* slots, int n_slots, int32_t* offsets, int per_agent,
+                                hipStream_t s) {
     const PageView v = page_view(p);
+    const FastDiv div = FastDiv::by(std::max(per_agent, 1));
     const int shared = 4 * v.A * (int)sizeof(int);
     if (shared > 48 * 1024) {   // (by call: the attribute belongs to the current device)
-        const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(pages_resize_kernel<1024>), hipFuncAttributeMaxDynamicSharedMemorySize, shared);
+        const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(pages_resize_kernel<1024, BY_AGENT>), hipFuncAttributeMaxDynamicSharedMemorySize, shared);
         if (err != hipSuccess) return err;
     }
     if (slots == nullptr) n_slots = 0;
     if (v.A <= 64 && n_slots <= 4096) {
-        launch_kernel(pages_resize_kernel<256>, dim3(1), dim3(256), shared, s, {}, v, targets, p->free_dev, p->free_state_dev, p->ticket_dev, slots,
-                      n_slots, offsets);
+        launch_kernel(pages_resize_kernel<256, BY_AGENT>, dim3(1), dim3(256), shared, s, {}, v, targets, p->free_dev, p->free_state_dev, p->ticket_dev, slots,
+                      n_slots, offsets, div);
     } else {
         const int by_slots = (n_slots + 4095) / 4096, by_agents = (v.A + 15) / 16;   // a round each: four slots a thread, an agent a wave
-        launch_kernel(pages_resize_kernel<1024>, dim3(min(max(by_slots, by_agents), 256)), dim3(1024), shared, s, {}, v, targets, p->free_dev,
-                      p->free_state_dev, p->ticket_dev, slots, n_slots, offsets);
+        launch_kernel(pages_resize_kernel<1024, BY_AGENT>, dim3(std::min(std::max(by_slots, by_agents), 256)), dim3(1024), shared, s, {}, v, targets, p->free_dev,
+                      p->free_state_dev, p->ticket_dev, slots, n_slots, offsets, div);
     }
     return hipGetLastError();
+}
+
+hipError_t launch_pages_resize(const polykv_pages* p, const int32_t* targets, int32_t* slots, int n_slots, int32_t* offsets,
+                               hipStream_t s) {
+    return launch_resize<false>(p, targets, slots, n_slots, offsets, 0, s);
+}
+hipError_t launch_pages_resize_by_agent(const polykv_pages* p, const int32_t* targets, int32_t* slots, int per_agent, int32_t* granted,
+                                        hipStream_t s) {
+    return launch_resize<true>(p, targets, slots, p->agents * per_agent, granted, per_agent, s);
 }
 
 // -------------------------------------------------------------------------------------- write ---

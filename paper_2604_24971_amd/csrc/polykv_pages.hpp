@@ -28,6 +28,8 @@ __device__ __forceinline__ int page_row(const PageView& v, int page, int h, int 
 
 hipError_t launch_pages_resize(const polykv_pages* p, const int32_t* targets, int32_t* slots, int n_slots, int32_t* offsets,
                                hipStream_t s);
+hipError_t launch_pages_resize_by_agent(const polykv_pages* p, const int32_t* targets, int32_t* slots, int per_agent, int32_t* granted,
+                                        hipStream_t s);
 hipError_t launch_pages_write(const polykv_pages* p, const void* K, const void* V, int in_dtype, int tokens, int64_t layer_stride,
                               int64_t token_stride, int64_t head_stride, const int32_t* slots, int layer_begin, int layer_end,
                               hipStream_t s);

@@ -2,6 +2,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <algorithm>
+
 #include "polykv_pages.hpp"
 
 namespace polykv {
@@ -64,6 +66,33 @@ static int check_nodes(int nodes, const char* who) {
         set_error("%s: nodes=%d must be in 1 .. %d", who, nodes, POLYKV_MAX_TREE_NODES);
         return POLYKV_ESHAPE;
     }
+    return POLYKV_OK;
+}
+
+// `sums`: the array that receives the offsets, or what was granted.
+static int check_resize(const polykv_pages* pages, const int32_t* targets, const int32_t* slots_dev, int slots, const int32_t* sums,
+                        const char* sums_name, const char* who) {
+    const int rc = check_pages(pages, false, who);
+    if (rc != POLYKV_OK) return rc;
+    if (pages->free_dev == nullptr || pages->free_state_dev == nullptr || pages->ticket_dev == nullptr || targets == nullptr) {
+        set_error("%s: NULL free list, ticket or targets", who);
+        return POLYKV_EINVAL;
+    }
+    if (!aligned(pages->free_dev, 4) || !aligned(pages->free_state_dev, 4) || !aligned(pages->ticket_dev, 4) || !aligned(targets, 4) || !aligned(slots_dev, 4) ||
+        !aligned(sums, 4)) {
+        set_error("%s: arrays must be 4-byte aligned", who);
+        return POLYKV_EINVAL;
+    }
+    if (slots_dev != nullptr && (slots < 0 || slots > (1 << 30))) {
+        set_error("%s: slots=%d outside [0, 2^30]", who, slots);
+        return POLYKV_ESHAPE;
+    }
+    const void* own[] = {pages->table_dev, pages->lengths_dev, pages->free_dev, pages->free_state_dev, pages->ticket_dev};
+    for (const void* p : own)
+        if (p == targets || p == slots_dev || p == sums || (slots_dev != nullptr && slots_dev == sums) || targets == slots_dev || targets == sums) {
+            set_error("%s: targets, slots and %s must be arrays of their own", who, sums_name);
+            return POLYKV_EINVAL;
+        }
     return POLYKV_OK;
 }
 
@@ -133,29 +162,22 @@ extern "C" {
 int polykv_pages_resize(const polykv_pages* pages, const int32_t* targets_dev, int32_t* slots_dev, int slots, int32_t* offsets_dev,
                         void* stream) {
     const char* who = "polykv_pages_resize";
-    const int rc = check_pages(pages, false, who);
+    const int rc = check_resize(pages, targets_dev, slots_dev, slots, offsets_dev, "offsets", who);
     if (rc != POLYKV_OK) return rc;
-    if (pages->free_dev == nullptr || pages->free_state_dev == nullptr || pages->ticket_dev == nullptr || targets_dev == nullptr) {
-        set_error("%s: NULL free list, ticket or targets", who);
-        return POLYKV_EINVAL;
-    }
-    if (!aligned(pages->free_dev, 4) || !aligned(pages->free_state_dev, 4) || !aligned(pages->ticket_dev, 4) || !aligned(targets_dev, 4) || !aligned(slots_dev, 4) ||
-        !aligned(offsets_dev, 4)) {
-        set_error("%s: arrays must be 4-byte aligned", who);
-        return POLYKV_EINVAL;
-    }
-    if (slots_dev != nullptr && (slots < 0 || slots > (1 << 30))) {
-        set_error("%s: slots=%d outside [0, 2^30]", who, slots);
+    return hip_result(launch_pages_resize(pages, targets_dev, slots_dev, slots, offsets_dev, (hipStream_t)stream), who);
+}
+
+int polykv_pages_resize_by_agent(const polykv_pages* pages, const int32_t* targets_dev, int32_t* slots_dev, int per_agent,
+                                 int32_t* granted_dev, void* stream) {
+    const char* who = "polykv_pages_resize_by_agent";
+    const int64_t slots = slots_dev != nullptr && pages != nullptr ? (int64_t)per_agent * std::max(pages->agents, 1) : 0;
+    if (slots > (1 << 30)) {   // (what else may be wrong with these numbers is looked at below)
+        set_error("%s: %d slots for each of %d agents are more than 2^30", who, per_agent, pages->agents);
         return POLYKV_ESHAPE;
     }
-    const void* own[] = {pages->table_dev, pages->lengths_dev, pages->free_dev, pages->free_state_dev, pages->ticket_dev};
-    for (const void* p : own)
-        if (p == targets_dev || p == slots_dev || p == offsets_dev || (slots_dev != nullptr && slots_dev == offsets_dev) ||
-            targets_dev == slots_dev || targets_dev == offsets_dev) {
-            set_error("%s: targets, slots and offsets must be arrays of their own", who);
-            return POLYKV_EINVAL;
-        }
-    return hip_result(launch_pages_resize(pages, targets_dev, slots_dev, slots, offsets_dev, (hipStream_t)stream), who);
+    const int rc = check_resize(pages, targets_dev, slots_dev, (int)std::max<int64_t>(slots, -1), granted_dev, "granted", who);
+    if (rc != POLYKV_OK) return rc;
+    return hip_result(launch_pages_resize_by_agent(pages, targets_dev, slots_dev, slots_dev != nullptr ? per_agent : 0, granted_dev, (hipStream_t)stream), who);
 }
 
 int polykv_pages_write(const polykv_pages* pages, const void* K_dev, const void* V_dev, int in_dtype, int tokens, int64_t layer_stride,

@@ -110,6 +110,8 @@ def _load():
     pp, tp, i64 = C.POINTER(PagesDesc), C.POINTER(TreeParams), C.c_int64
     lib.polykv_pages_resize.argtypes = [pp, vp, vp, ip, vp, vp]
     lib.polykv_pages_resize.restype = ip
+    lib.polykv_pages_resize_by_agent.argtypes = [pp, vp, vp, ip, vp, vp]
+    lib.polykv_pages_resize_by_agent.restype = ip
     lib.polykv_pages_write.argtypes = [pp, vp, vp, ip, ip, i64, i64, i64, vp, ip, ip, vp]
     lib.polykv_pages_write.restype = ip
     lib.polykv_tree_masks.argtypes = [vp, vp, ip, ip, vp, vp, vp]
@@ -505,15 +507,33 @@ class Pages:
         self._per_agent, self._per_offset = self.lengths.shape, torch.Size((agents + 1,))
         self._workspaces = {}   # stream handle -> cached attend_tree workspace
 
-    # polykv_pages_resize(targets, slots, offsets)
-    def resize(self, targets: torch.Tensor, slots: torch.Tensor | None = None, offsets: torch.Tensor | None = None, stream=None):
+    # polykv_pages_resize(targets, slots, offsets), polykv_pages_resize_by_agent(targets, slots, granted)
+    def resize(self, targets: torch.Tensor, slots: torch.Tensor | None = None, offsets: torch.Tensor | None = None, stream=None, *,
+               granted: torch.Tensor | None = None):
         """Agent a's continuation becomes targets[a] tokens long: pages are taken for it or given back.  An agent for which
         there are no pages, or whose target is out of range, keeps its length.  `slots` (int32, any length) receives the
         places of the tokens that agents grew by, for write(), agent after agent, and -1 behind them; `offsets` (int32
-        [agents + 1]) where each agent's begin."""
+        [agents + 1]) where each agent's begin.
+
+        With `granted` (int32 [agents]) places go by agent: `slots` is [agents, n], entry [a, i] the place of the i-th token
+        that agent a grew by and -1 behind them, and granted[a] receives how many these are.  For rows of drafts [agents, n]
+        this is the form to use: write() takes slots.view(-1), and tree_masks(), attend_tree() and accept() take `granted`
+        as their counts, so that an agent that kept its length has no drafts in the step."""
         if _elsewhere(self._index):
             with torch.cuda.device(self._index):
-                return self.resize(targets, slots, offsets, stream)
+                return self.resize(targets, slots, offsets, stream, granted=granted)
+        if granted is not None:
+            if offsets is not None:
+                raise ValueError("offsets are those of slots without granted")
+            n = 0
+            if slots is not None:
+                if slots.dim() != 2:
+                    raise ValueError("with granted, slots must be [agents, n]")
+                n = slots.shape[1]
+                slots = _ints(slots, (self.agents, n), self.device, "slots")
+            _check(lib.polykv_pages_resize_by_agent(self._ref, _ints(targets, self._per_agent, self.device, "targets"), slots, n,
+                                                    _ints(granted, self._per_agent, self.device, "granted"), _stream_ptr(stream)))
+            return
         n = 0
         if slots is not None:
             n = slots.numel()

@@ -168,3 +168,20 @@ def test_a_closed_pool_is_not_an_absent_one():
         with pytest.raises(pk.PolyKVError) as e:
             call()
         assert e.value.status == pk.EINVAL and "closed" in str(e.value)
+
+
+def test_resize_by_agent_refusals():
+    d = C.byref(desc())
+    f = lib.polykv_pages_resize_by_agent
+    a, b, c = (C.c_void_p(0x40000 + 0x1000 * k) for k in range(3))
+    for bad, code in BAD_PAGES:
+        assert f(C.byref(desc(**bad)), a, b, 4, c, None) == code
+    assert f(None, a, b, 4, c, None) == pk.EINVAL and f(d, None, b, 4, c, None) == pk.EINVAL
+    for args in ((C.c_void_p(0x20000), b, 4, c), (a, P, 4, c), (a, b, 4, P), (P, b, 4, c), (a, a, 4, c), (a, b, 4, a), (a, b, 4, b), (a, b, 4, C.c_void_p(0x20000))):
+        assert f(d, *args, None) == pk.EINVAL                               # arrays that are also something else
+    assert f(d, C.c_void_p(0x10002), b, 4, c, None) == pk.EINVAL and f(d, a, b, 4, C.c_void_p(0x40001), None) == pk.EINVAL
+    for per_agent in (-1, -2 ** 31, 2 ** 30 // 3 + 1, 2 ** 31 - 1):
+        assert f(d, a, b, per_agent, c, None) == pk.ESHAPE
+    assert f(C.byref(desc(free_dev=None)), a, b, 4, c, None) == pk.EINVAL
+    assert f(C.byref(desc(free_state_dev=None)), a, b, 4, c, None) == pk.EINVAL
+    assert f(C.byref(desc(ticket_dev=None)), a, b, 4, c, None) == pk.EINVAL
