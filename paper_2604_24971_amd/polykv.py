@@ -426,6 +426,14 @@ def _elsewhere(index: int) -> bool:
     return (_get_device() if _get_device is not None and torch.cuda.is_initialized() else torch.cuda.current_device()) != index
 
 
+def _capturing(stream=None) -> bool:
+    """Whether the stream that the call runs on is being captured, which need not be the current one."""
+    if stream is None:
+        return torch.cuda.is_current_stream_capturing()
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
 def _new(shape, dtype, device, stream=None):
     """A tensor from the memory of the stream that the call runs on."""
     if stream is None:
@@ -603,7 +611,7 @@ class Pages:
         # One cached workspace per stream: calls on different streams may overlap and must not share one.  A call that is
         # being captured gets one of its own from the graph's memory: graphs may be replayed on any streams.
         own = workspace is None
-        capturing = own and torch.cuda.is_current_stream_capturing()
+        capturing = own and _capturing(stream)
         ws = workspace if not own else None if capturing else self._workspaces.get(sp)
         if ws is not None:
             p.workspace_dev, p.workspace_bytes = ws.data_ptr() if own else _dev_ptr(ws, torch.uint8, "workspace"), ws.numel()

@@ -801,3 +801,38 @@ def test_on_another_stream_and_twice():
     got = [pool.attend_tree(Q, s.pages, page_splits=2, stream=side) for _ in range(3)]
     side.synchronize()
     assert all(torch.equal(want, x) for x in got)
+
+
+def test_a_captured_stream_that_is_not_the_current_one():
+    """A call on a stream by name, which is being captured while another is current: the graph has a workspace of its own, and its
+    replays leave alone the one of that stream's eager calls."""
+    rng = np.random.default_rng(6)
+    s = Setup(rng, [300, 10, 64], 128, L=2)
+    pool, _ = _pool(rng, 2, 2, 128, 900, F16)
+    Q, other_Q = (dev(rng.standard_normal((2, 3, 4, 8, 128)), F16) for _ in range(2))
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    for known in (True, False):       # with and without an eager workspace of the stream
+        s.pages._workspaces.clear()
+        want = pool.attend_tree(Q, s.pages, page_splits=2)
+        torch.cuda.synchronize()
+        if known:
+            pool.attend_tree(Q, s.pages, page_splits=2, stream=side)
+            torch.cuda.synchronize()
+        graph, out = torch.cuda.CUDAGraph(), torch.zeros_like(Q)
+        with torch.cuda.stream(side):
+            graph.capture_begin()
+            with torch.cuda.stream(other):
+                pool.attend_tree(Q, s.pages, out, page_splits=2, stream=side)
+            graph.capture_end()
+        pool.attend_tree(other_Q, s.pages, page_splits=2, stream=side)
+        torch.cuda.synchronize()
+        eager = s.pages._workspaces[side.cuda_stream]
+        eager.fill_(0x5C)
+        for _ in range(3):
+            out.zero_()
+            torch.cuda.synchronize()
+            with torch.cuda.stream(other):
+                graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want)
+            assert bool((eager == 0x5C).all())
