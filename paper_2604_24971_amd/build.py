@@ -37,12 +37,13 @@ def _run(cmd):
 def _check_no_scratch(remarks: str):
     """The matrix-core attention kernel keeps its accumulators, parked query operands and score tiles in all 512
     registers of a wave; builds in which the register allocator spilled part of that to scratch memory returned
-    wrong results on the GPU.  Refuse such a build: every instantiation must come out without scratch."""
+    wrong results on the GPU.  Refuse such a build: every instantiation must come out without scratch.  The same for the kernels
+    over pages, some of which fill their registers to the last few: a spill in their loops is only slow, but nothing else shows it."""
     name = None
     for line in remarks.splitlines():
         if "Function Name:" in line:
             name = line.split("Function Name:")[1].split()[0]
-        elif "ScratchSize" in line and name and "attend_mfma_" in name:
+        elif "ScratchSize" in line and name and any(kernel in name for kernel in ("attend_mfma_", "attend_pages_")):
             size = int(line.split("ScratchSize [bytes/lane]:")[1].split()[0])
             if size and not os.environ.get("POLYKV_BUILD_ALLOW_SCRATCH"):   # (the variable is for timing experiments only)
                 raise RuntimeError("%s spills %d bytes per lane to scratch: reduce its register use" % (name, size))
@@ -171,6 +172,10 @@ def build_library(verbose: bool = True, extra_flags=()) -> str:
             log = _run(cmd + ["-Rpass-analysis=kernel-resource-usage", "-fno-caret-diagnostics", "-save-temps=obj"])
             _check_no_scratch(log)
             _check_wait_states(os.path.join(objdir, "polykv_attend_mfma-hip-amdgcn-amd-amdhsa-gfx950.s"))
+            return "\n".join(l for l in log.splitlines() if "kernel-resource-usage" not in l)
+        if SOURCES[i] == "polykv_tree.hip":
+            log = _run(cmd + ["-Rpass-analysis=kernel-resource-usage", "-fno-caret-diagnostics"])
+            _check_no_scratch(log)
             return "\n".join(l for l in log.splitlines() if "kernel-resource-usage" not in l)
         return _run(cmd)
 

@@ -337,24 +337,28 @@ template <int D> struct PoolSums {
     }
     // d += the value sums of a row's splits, each times 2^(m - M) * scale; coordinates base + at(i) .. + 3 in d[4 i] .. d[4 i + 3].
     template <int N, class At> __device__ static __forceinline__ void add(const TreeArgs& g, const Place& p, int r, float M, float scale, float (&d)[N], At at) {
-        auto splits = [&](int s0, auto count) {   // all are requested before the first is used
+        constexpr int PIECE = N < 128 ? N / 4 : N / 8;   // (as far as the registers reach: all of 128 took 68 bytes of scratch a lane)
+        auto splits = [&](int s0, auto count) {   // all of a piece are requested before the first is used
             constexpr int B = decltype(count)::value;
-            float4 z[B][N / 4];
-            float w[B];
 #pragma unroll
-            for (int k = 0; k < B; ++k) {
-                w[k] = load(g, p, r, s0 + k).x;
-                const float* src = g.pool.o + row(g, p, r, s0 + k) * D;
+            for (int i0 = 0; i0 < N / 4; i0 += PIECE) {
+                float4 z[B][PIECE];
+                float w[B];
 #pragma unroll
-                for (int i = 0; i < N / 4; ++i) z[k][i] = *reinterpret_cast<const float4*>(src + at(i));
-            }
+                for (int k = 0; k < B; ++k) {
+                    w[k] = load(g, p, r, s0 + k).x;
+                    const float* src = g.pool.o + row(g, p, r, s0 + k) * D;
 #pragma unroll
-            for (int k = 0; k < B; ++k) {
-                const float f = __builtin_amdgcn_exp2f(w[k] - M) * scale;
+                    for (int i = 0; i < PIECE; ++i) z[k][i] = *reinterpret_cast<const float4*>(src + at(i0 + i));
+                }
 #pragma unroll
-                for (int i = 0; i < N / 4; ++i) {
-                    float* y = d + 4 * i;
-                    y[0] = fmaf(z[k][i].x, f, y[0]), y[1] = fmaf(z[k][i].y, f, y[1]), y[2] = fmaf(z[k][i].z, f, y[2]), y[3] = fmaf(z[k][i].w, f, y[3]);
+                for (int k = 0; k < B; ++k) {
+                    const float f = __builtin_amdgcn_exp2f(w[k] - M) * scale;
+#pragma unroll
+                    for (int i = 0; i < PIECE; ++i) {
+                        float* y = d + 4 * (i0 + i);
+                        y[0] = fmaf(z[k][i].x, f, y[0]), y[1] = fmaf(z[k][i].y, f, y[1]), y[2] = fmaf(z[k][i].z, f, y[2]), y[3] = fmaf(z[k][i].w, f, y[3]);
+                    }
                 }
             }
         };
@@ -461,8 +465,9 @@ __global__ __launch_bounds__(SHARE ? 256 : 64, few_waves_per_simd(D, R)) void at
     using S = Shape<D, R>;
     constexpr int MG = S::MG, KJ = S::KJ, SN = S::SN, VW = MG / 2, OSTRIDE = D + 4, STEP = SHARE ? 4 : 1;
     // Head_dim 256: a tile's keys and values and the sums leave no registers for the queries, which wait in LDS (8 layers x 8 heads x 50
-    // agents over 300 tokens 143 us, 161 with them in registers and 60 bytes a lane of addresses in scratch).
-    constexpr bool Q_LDS = D == 256;
+    // agents over 300 tokens 143 us, 161 with them in registers and 60 bytes a lane of addresses in scratch).  At 128 the bfloat16 form whose
+    // four waves share sixteen rows lacks two registers (12 bytes of scratch, reloaded in every tile; times within 0.5 % either way).
+    constexpr bool Q_LDS = D == 256 || (SHARE && BF && D == 128 && R == 16);
     __shared__ tree_uint4 q_own[Q_LDS && !SHARE ? KJ * 64 : 1];
     extern __shared__ __align__(16) float o_s[];   // [4][R][OSTRIDE] (SHARE)
     __shared__ float m_s[SHARE ? 4 : 1][R], l_s[SHARE ? 4 : 1][R];

@@ -38,3 +38,12 @@ def test_distances_that_are_kept(tmp_path):
 def test_distances_that_are_too_short(tmp_path, lines, what):
     with pytest.raises(RuntimeError, match=what):
         _check(tmp_path, *lines)
+
+
+@pytest.mark.parametrize("kernel", ["_ZN6polykv18attend_mfma_kernelILi128EEEvPKh", "_ZN6polykv24attend_pages_many_kernelILi256ELb1ELi4EEEvNS_8TreeArgsE",
+                                    "_ZN6polykv23attend_pages_few_kernelILi128ELb1ELi16ELb1EEEvNS_8TreeArgsE"])
+def test_scratch_is_refused(kernel):
+    remarks = "x.hip:1:1: remark: Function Name: %s [-Rpass]\nx.hip:1:1: remark:     ScratchSize [bytes/lane]: %d [-Rpass]\n"
+    build._check_no_scratch(remarks % (kernel, 0))
+    with pytest.raises(RuntimeError, match="12 bytes"):
+        build._check_no_scratch(remarks % (kernel, 12))
