@@ -58,41 +58,41 @@ template <int D> static int tile_bytes_of(int vc, int kc) {
 
 // Resolve every choice pool_attend makes from the pool shape and the caller's parameters, so that
 // pool_attend_workspace() and pool_attend() agree by construction.
-int make_plan(const polykv_pool* pool, const polykv_attend_params* prm, AttendPlan* plan) {
+int make_plan(const polykv_pool* pool, const polykv_attend_params* prm, AttendPlan* plan, const char* who) {
     if (pool == nullptr || prm == nullptr) {
-        set_error("pool_attend: NULL pool or params");
+        set_error("%s: NULL pool or params", who);
         return POLYKV_EINVAL;
     }
     if (prm->agents < 1 || prm->q_per_agent < 1 || prm->q_heads < 1 || prm->q_heads % pool->kv_heads != 0) {
-        set_error("pool_attend: agents=%d q_per_agent=%d q_heads=%d must be >= 1 and q_heads a multiple of kv_heads=%d",
+        set_error("%s: agents=%d q_per_agent=%d q_heads=%d must be >= 1 and q_heads a multiple of kv_heads=%d", who,
                   prm->agents, prm->q_per_agent, prm->q_heads, pool->kv_heads);
         return POLYKV_ESHAPE;
     }
     if (prm->layer_begin < 0 || prm->layer_end > pool->layers || prm->layer_begin >= prm->layer_end) {
-        set_error("pool_attend: layer range [%d,%d) outside [0,%d)", prm->layer_begin, prm->layer_end, pool->layers);
+        set_error("%s: layer range [%d,%d) outside [0,%d)", who, prm->layer_begin, prm->layer_end, pool->layers);
         return POLYKV_ESHAPE;
     }
     if (prm->kernel < POLYKV_KERNEL_AUTO || prm->kernel > POLYKV_KERNEL_MATRIX || prm->splits < 0) {
-        set_error("pool_attend: bad kernel selector %d or splits %d", prm->kernel, prm->splits);
+        set_error("%s: bad kernel selector %d or splits %d", who, prm->kernel, prm->splits);
         return POLYKV_EINVAL;
     }
     const bool tails = prm->tail_len != nullptr;
     if (tails) {
         if (prm->tail_K == nullptr || prm->tail_V == nullptr) {
-            set_error("pool_attend: tail_len given without tail_K/tail_V");
+            set_error("%s: tail_len given without tail_K/tail_V", who);
             return POLYKV_EINVAL;
         }
         if (prm->agents > POLYKV_MAX_TAIL_AGENTS) {
-            set_error("pool_attend: tails support at most %d agents", POLYKV_MAX_TAIL_AGENTS);
+            set_error("%s: tails support at most %d agents", who, POLYKV_MAX_TAIL_AGENTS);
             return POLYKV_ESHAPE;
         }
         for (int a = 0; a < prm->agents; ++a) {
             if (prm->tail_len[a] < 0 || prm->tail_len[a] > prm->tail_capacity) {
-                set_error("pool_attend: tail_len[%d]=%d outside [0, tail_capacity=%d]", a, prm->tail_len[a], prm->tail_capacity);
+                set_error("%s: tail_len[%d]=%d outside [0, tail_capacity=%d]", who, a, prm->tail_len[a], prm->tail_capacity);
                 return POLYKV_ESHAPE;
             }
             if (prm->tail_len[a] > 0 && (prm->tail_K[a] == nullptr || prm->tail_V[a] == nullptr)) {
-                set_error("pool_attend: agent %d has tail_len > 0 but a NULL tail pointer", a);
+                set_error("%s: agent %d has tail_len > 0 but a NULL tail pointer", who, a);
                 return POLYKV_EINVAL;
             }
         }
@@ -117,12 +117,12 @@ int make_plan(const polykv_pool* pool, const polykv_attend_params* prm, AttendPl
     p.G = prm->q_heads / pool->kv_heads;
     const long rows = (long)p.A * p.nq * p.G;
     if (rows > (1 << 20)) {
-        set_error("pool_attend: %ld query rows per KV head is more than supported", rows);
+        set_error("%s: %ld query rows per KV head is more than supported", who, rows);
         return POLYKV_ESHAPE;
     }
     p.R = (int)rows;
     if (!(prm->scale >= 0.0f) || !(prm->scale <= 3.0e38f)) {
-        set_error("pool_attend: the softmax scale must be finite and >= 0 (0 = 1/sqrt(head_dim))");
+        set_error("%s: the softmax scale must be finite and >= 0 (0 = 1/sqrt(head_dim))", who);
         return POLYKV_EINVAL;
     }
     const float scale = prm->scale != 0.0f ? prm->scale : 1.0f / sqrtf((float)p.D);
@@ -131,29 +131,29 @@ int make_plan(const polykv_pool* pool, const polykv_attend_params* prm, AttendPl
     p.tail_capacity = tails ? prm->tail_capacity : 0;
     p.tail_causal = (tails && prm->tail_causal != 0) ? 1 : 0;
     if (prm->io_dtype != POLYKV_F16 && prm->io_dtype != POLYKV_BF16) {
-        set_error("pool_attend: io_dtype %d is neither POLYKV_F16 nor POLYKV_BF16", prm->io_dtype);
+        set_error("%s: io_dtype %d is neither POLYKV_F16 nor POLYKV_BF16", who, prm->io_dtype);
         return POLYKV_EINVAL;
     }
     p.io_bf16 = prm->io_dtype == POLYKV_BF16 ? 1 : 0;
     if (prm->key_precision != POLYKV_KEY_PRECISION_EXACT && prm->key_precision != POLYKV_KEY_PRECISION_FP16) {
-        set_error("pool_attend: key_precision %d is not a POLYKV_KEY_PRECISION_* value", prm->key_precision);
+        set_error("%s: key_precision %d is not a POLYKV_KEY_PRECISION_* value", who, prm->key_precision);
         return POLYKV_EINVAL;
     }
     p.signs = pool->signs;
 
     const bool mat_ok = matrix_kernel_supports(p.D, p.vcodec);
     if (prm->kernel == POLYKV_KERNEL_MATRIX && !mat_ok) {
-        set_error("pool_attend: the matrix-core kernel does not support int8 values at head_dim=%d", p.D);
+        set_error("%s: the matrix-core kernel does not support int8 values at head_dim=%d", who, p.D);
         return POLYKV_ESHAPE;
     }
     p.kernel = prm->kernel != POLYKV_KERNEL_AUTO ? prm->kernel : mat_ok ? POLYKV_KERNEL_MATRIX : POLYKV_KERNEL_VECTOR;
     // Launch limits: the vector kernel and the tail kernel put their 4-row blocks on grid.z (at most 65,535).
     if (p.kernel == POLYKV_KERNEL_VECTOR && (p.R + 3) / 4 > 65535) {
-        set_error("pool_attend: the vector kernel supports at most 262,140 query rows per KV head (got %d)", p.R);
+        set_error("%s: the vector kernel supports at most 262,140 query rows per KV head (got %d)", who, p.R);
         return POLYKV_ESHAPE;
     }
     if (tails && ((long)p.nq * p.G + 3) / 4 > 65535) {
-        set_error("pool_attend: with tails, q_per_agent * (q_heads / kv_heads) = %ld exceeds 262,140", (long)p.nq * p.G);
+        set_error("%s: with tails, q_per_agent * (q_heads / kv_heads) = %ld exceeds 262,140", who, (long)p.nq * p.G);
         return POLYKV_ESHAPE;
     }
     p.key_fp16 = (prm->key_precision == POLYKV_KEY_PRECISION_FP16 && p.kernel == POLYKV_KERNEL_MATRIX &&
@@ -525,13 +525,13 @@ int pool_export_value_scales(const polykv_pool* pool, void* v_scales_dev, void* 
 
 size_t pool_attend_workspace(const polykv_pool* pool, const polykv_attend_params* params) {
     AttendPlan plan;
-    if (make_plan(pool, params, &plan) != POLYKV_OK) return 0;
+    if (make_plan(pool, params, &plan, "pool_attend") != POLYKV_OK) return 0;
     return plan.total;
 }
 
 int pool_attend_plan(const polykv_pool* pool, const polykv_attend_params* params, polykv_attend_choice* choice) {
     AttendPlan plan;
-    const int rc = make_plan(pool, params, &plan);
+    const int rc = make_plan(pool, params, &plan, "pool_attend");
     if (rc != POLYKV_OK) return rc;
     if (choice == nullptr) {
         set_error("pool_attend_plan: NULL choice");
@@ -558,7 +558,7 @@ int pool_attend(const polykv_pool* pool, const void* Q_dev, void* out_dev, const
     int rc = check_readable(pool, "pool_attend");
     if (rc != POLYKV_OK) return rc;
     AttendPlan plan;
-    rc = make_plan(pool, params, &plan);
+    rc = make_plan(pool, params, &plan, "pool_attend");
     if (rc != POLYKV_OK) return rc;
     if (params->workspace_dev == nullptr || ((uintptr_t)params->workspace_dev & 255) != 0) {
         set_error("pool_attend: workspace must be a 256-byte aligned device pointer");
@@ -609,7 +609,7 @@ int pool_attend_static(const polykv_pool* pool, const void* Q_dev, void* out_dev
     int rc = check_readable(pool, "pool_attend_static");
     if (rc != POLYKV_OK) return rc;
     AttendPlan plan;
-    rc = make_plan(pool, params, &plan);
+    rc = make_plan(pool, params, &plan, "pool_attend");
     if (rc != POLYKV_OK) return rc;
     if (plan.total > (size_t)POLYKV_STATIC_WORKSPACE_BYTES) {
         set_error("pool_attend_static: this call needs %zu bytes of scratch, the built-in buffer holds %zu; use "

@@ -87,7 +87,7 @@ hipError_t launch_decode(const polykv_pool* p, void* K_out, void* V_out, int dty
                          hipStream_t s);
 hipError_t launch_export(const polykv_pool* p, void* kc, void* ks, void* vp, void* vs, hipStream_t s);
 // Resolves every choice of a pool_attend call and validates its parameters; the reason of a refusal is in the error text.
-int make_plan(const polykv_pool* pool, const polykv_attend_params* prm, AttendPlan* plan);
+int make_plan(const polykv_pool* pool, const polykv_attend_params* prm, AttendPlan* plan, const char* who);
 int check_readable(const polykv_pool* pool, const char* who);
 int hip_result(hipError_t e, const char* who);
 hipError_t launch_attend(const polykv_pool* p, const AttendPlan& plan, const void* Q, void* out,

@@ -124,7 +124,7 @@ static int make_tree_plan(const polykv_pool* pool, const polykv_pages* pages, co
     polykv_pool none;   // without a pool: the same checks, for a pool of one empty tile
     memset(&none, 0, sizeof(none));
     none.layers = pages->layers, none.kv_heads = pages->kv_heads, none.head_dim = pages->head_dim, none.tokens = 1, none.tiles = 1;
-    rc = make_plan(pool != nullptr ? pool : &none, &a, plan);
+    rc = make_plan(pool != nullptr ? pool : &none, &a, plan, who);
     if (rc != POLYKV_OK) return rc;
     plan->partials_only = 1;
     TreePlan& t = *tree;

@@ -185,3 +185,17 @@ def test_resize_by_agent_refusals():
     assert f(C.byref(desc(free_dev=None)), a, b, 4, c, None) == pk.EINVAL
     assert f(C.byref(desc(free_state_dev=None)), a, b, 4, c, None) == pk.EINVAL
     assert f(C.byref(desc(ticket_dev=None)), a, b, 4, c, None) == pk.EINVAL
+
+
+def test_refusals_name_the_call():
+    """Also those of the planner that pool_attend and pool_attend_tree share."""
+    d = C.byref(desc())
+    for bad in (dict(scale=-1.0), dict(q_heads=3), dict(kernel=9), dict(layer_end=3), dict(key_precision=5)):
+        p = C.byref(params(workspace_dev=0x100000, workspace_bytes=1 << 40, **bad))
+        assert lib.pool_attend_tree(None, d, P, P, p, None) != pk.OK
+        assert lib.polykv_last_error().startswith(b"pool_attend_tree: "), bad
+    h = C.c_void_p()
+    assert lib.pool_create(2, 2, 64, 100, C.byref(h)) == pk.OK
+    a = pk.AttendParams(agents=1, q_per_agent=1, q_heads=3, layer_end=2)
+    assert lib.pool_attend_workspace(h, C.byref(a)) == 0 and lib.polykv_last_error().startswith(b"pool_attend: ")
+    lib.pool_destroy(h)
