@@ -49,7 +49,7 @@ struct TreePlan {
     int nsplit;                // token-range splits of the pages' part
     int merge;                 // 1: the pages' kernel writes partials for the merge kernel, 0: the output
     int wave_rows;             // rows of a wave: 32, or 16 (waves == 1)
-    int waves;                 // waves with rows of their own in a workgroup: 1 .. 4
+    int waves;                 // waves with rows of their own in a workgroup: 1, 2 or 4
     int share;                 // 1 (waves == 1): four waves share the rows
     int row_blocks;            // blocks of rows of an agent and KV head
     FastDiv div_H, div_A, div_G, div_nsplit, div_row_blocks;

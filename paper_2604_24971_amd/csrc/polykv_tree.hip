@@ -795,8 +795,7 @@ __global__ __launch_bounds__(64 * W, many_waves_per_simd(D)) void attend_pages_m
         };
         fetch_pages(t_begin);
         ask(t_begin, Set<0>());
-        if constexpr (SETS > 1) ask(t_begin + 1, Set<1 % SETS>());
-        if constexpr (SETS > 2) ask(t_begin + 2, Set<2 % SETS>());
+        if constexpr (SETS > 1) ask(t_begin + 1, Set<1>());
         tree_uint4 q[KJ];
         const int draft = load_queries<D, R>(g, pl, my_row0, lane, q);
         const uint64_t see_first = first_drafts(t, pl, draft);
@@ -846,9 +845,7 @@ __global__ __launch_bounds__(64 * W, many_waves_per_simd(D)) void attend_pages_m
         for (int tile = t_begin; tile < t_end; tile += SETS) {
             step(tile, Set<1 % SETS>());
             if constexpr (SETS > 1)
-                if (tile + 1 < t_end) step(tile + 1, Set<2 % SETS>());
-            if constexpr (SETS > 2)
-                if (tile + 2 < t_end) step(tile + 2, Set<0>());
+                if (tile + 1 < t_end) step(tile + 1, Set<0>());
         }
         rows.l += poison;
     }
