@@ -373,10 +373,12 @@ class Pool:
         p, _keep = self._params(Q, q_heads, layer_begin, layer_end, scale, tails, kernel, splits, tail_causal,
                                 key_precision)
         sp = _stream_ptr(stream)
-        # one cached workspace per stream: calls on different streams may overlap and must not share one
-        ws = workspace if workspace is not None else self._workspaces.get(sp)
+        # One cached workspace per stream: calls on different streams may overlap and must not share one.  A call that is being
+        # captured gets one of its own from the graph's memory: graphs may be replayed on any streams.
+        capturing = workspace is None and _capturing(stream)
+        ws = workspace if workspace is not None else None if capturing else self._workspaces.get(sp)
         if ws is None:
-            ws = self._grow_workspace(p, sp, stream)
+            ws = self._grow_workspace(p, sp, stream, keep=not capturing)
         p.workspace_dev = _dev_ptr(ws, torch.uint8, "workspace")
         p.workspace_bytes = ws.numel()
         if out is None:
@@ -390,14 +392,16 @@ class Pool:
         _check(rc)
         return out
 
-    def _grow_workspace(self, p, sp, stream):
+    def _grow_workspace(self, p, sp, stream, keep=True):
         need = lib.pool_attend_workspace(self._h, C.byref(p))
         if need == 0:
             _check(lib.pool_attend(self._h, None, None, C.byref(p), None))  # surfaces the shape error
         # From the memory of the stream that uses it: the one it replaces may still be in use there, and goes to later work of
         # that stream only.
         with torch.cuda.stream(stream):
-            ws = self._workspaces[sp] = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
+            ws = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
+        if keep:
+            self._workspaces[sp] = ws
         return ws
 
     # pool_attend_static(Q[agents], out): no workspace, nothing allocated by the library

@@ -77,3 +77,36 @@ def test_a_replaced_workspace_stays_with_its_stream():
     others = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in range(64)]
     assert pool._workspaces[side.cuda_stream].data_ptr() != at and all(t.data_ptr() != at for t in others)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("other_current", [False, True])
+def test_captured_calls_have_workspaces_of_their_own(other_current):
+    """A graph may be replayed on any stream, and the eager workspace of the stream it was captured on may be replaced: its replays
+    neither use nor need that one."""
+    pool, small, large = _pool()
+    want_small, want_large = pool.attend(small, splits=2), pool.attend(large, splits=4)
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    pool.attend(large, splits=4, stream=side)
+    torch.cuda.synchronize()
+    eager = pool._workspaces[side.cuda_stream]
+    graphs = []
+    for Q, splits, want in ((small, 2, want_small), (large, 4, want_large)):
+        graph, out = torch.cuda.CUDAGraph(), torch.zeros_like(want)
+        with torch.cuda.stream(side):
+            graph.capture_begin()
+            with torch.cuda.stream(other if other_current else side):
+                pool.attend(Q, out, splits=splits, stream=side)
+            graph.capture_end()
+        graphs.append((graph, out, want))
+    assert pool._workspaces[side.cuda_stream] is eager
+    eager.fill_(0x5C)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for (graph, out, want), stream in zip(graphs, (side, other)):
+            out.zero_()
+            torch.cuda.synchronize()
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(out, want) for _, out, want in graphs)
+        assert bool((eager == 0x5C).all())
