@@ -352,7 +352,7 @@ typedef struct {
 size_t pool_attend_tree_workspace(const polykv_pool* pool, const polykv_pages* pages, const polykv_tree_params* params);
 
 /* Q_dev: [layer_end - layer_begin, agents, nodes, q_heads, head_dim] of the pages' type; out_dev: the same shape and
- * type (fp32 results rounded once, to nearest even).  Draft i of agent a attends the pool's tokens (pool NULL: there is
+ * type (fp32 results rounded once, to nearest even), Q_dev itself or memory that does not overlap it.  Draft i of agent a attends the pool's tokens (pool NULL: there is
  * none), the agent's tokens before its drafts, and those of its drafts that its mask names.  Rows from counts[a] on
  * attend the pool alone; a row that sees nothing gets zeros.  The pool's head_dim, layers and kv_heads must be the pages'.
  * A token that a draft does not see has no effect on it, whatever its vectors hold; a draft that sees a drafted token

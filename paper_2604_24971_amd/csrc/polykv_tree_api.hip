@@ -255,6 +255,13 @@ int pool_attend_tree(const polykv_pool* pool, const polykv_pages* pages, const v
         set_error("%s: Q and out must be 16-byte aligned device pointers", who);
         return POLYKV_EINVAL;
     }
+    // (in place is fine: rows are read by the workgroups that write them, before they do; other rows need not be)
+    const uintptr_t q = (uintptr_t)Q_dev, o_at = (uintptr_t)out_dev;
+    const size_t q_bytes = (size_t)plan.layers * plan.H * plan.R * plan.D * 2;
+    if (q != o_at && q < o_at + q_bytes && o_at < q + q_bytes) {
+        set_error("%s: out must be Q itself or not overlap it", who);
+        return POLYKV_EINVAL;
+    }
     if (!aligned(params->counts_dev, 4) || !aligned(params->mask_dev, 8)) {
         set_error("%s: counts must be 4-byte and mask 8-byte aligned", who);
         return POLYKV_EINVAL;

@@ -836,3 +836,24 @@ def test_a_captured_stream_that_is_not_the_current_one():
             torch.cuda.synchronize()
             assert torch.equal(out, want)
             assert bool((eager == 0x5C).all())
+
+
+@pytest.mark.parametrize("d,nodes,group,layers", [(64, 4, 2, 1), (128, 40, 4, 1), (64, 8, 2, 100), (128, 20, 1, 100), (128, 20, 2, 100), (256, 3, 2, 100), (256, 90, 2, 60)])
+@pytest.mark.parametrize("page_splits", [1, 2])
+def test_in_place(d, nodes, group, layers, page_splits):
+    """The output may be the queries themselves, in every form, with and without a pool."""
+    rng = np.random.default_rng(d + nodes)
+    pages = _pk().Pages(layers, 2, d, 60, 3, 20, dtype=F16)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for x in (pages.K, pages.V):
+        x.normal_(generator=g)
+    pages.table.copy_(dev(rng.permutation(60).astype(np.int32)).view(3, 20))
+    pages.lengths.copy_(dev(np.array([310, nodes, 150], np.int32)))
+    Q = torch.randn((layers, 3, nodes, 2 * group, d), device="cuda", generator=g).half()
+    pool = _pk().Pool(layers, 2, d, 200).bind()
+    pool.encode(*(torch.randn((layers, 2, 200, d), device="cuda", generator=g).half() for _ in range(2)))
+    for call in (pages.attend_tree, lambda q, out, **kw: pool.attend_tree(q, pages, out, **kw)):
+        want = call(Q, torch.empty_like(Q), page_splits=page_splits)
+        both = Q.clone()
+        assert call(both, both, page_splits=page_splits) is both
+        assert torch.equal(both, want)

@@ -199,3 +199,16 @@ def test_refusals_name_the_call():
     a = pk.AttendParams(agents=1, q_per_agent=1, q_heads=3, layer_end=2)
     assert lib.pool_attend_workspace(h, C.byref(a)) == 0 and lib.polykv_last_error().startswith(b"pool_attend: ")
     lib.pool_destroy(h)
+
+
+def test_out_that_overlaps_the_queries():
+    d = C.byref(desc(max_blocks=64))
+    nbytes = 2 * 3 * 4 * 4 * 64 * 2       # layers, agents, drafts, query heads, head_dim
+    p = C.byref(params(page_splits=4, workspace_dev=0x100000, workspace_bytes=0))
+    at = lambda k: C.c_void_p(0x4000000 + k)  # noqa: E731
+    for k in (16, nbytes - 16):
+        assert lib.pool_attend_tree(None, d, at(0), at(k), p, None) == pk.EINVAL and b"overlap" in lib.polykv_last_error()
+        assert lib.pool_attend_tree(None, d, at(k), at(0), p, None) == pk.EINVAL and b"overlap" in lib.polykv_last_error()
+    for k in (0, nbytes):                  # (in place, and side by side: the workspace is what is refused)
+        assert lib.pool_attend_tree(None, d, at(0), at(k), p, None) == pk.ENOMEM
+        assert lib.pool_attend_tree(None, d, at(k), at(0), p, None) == pk.ENOMEM
