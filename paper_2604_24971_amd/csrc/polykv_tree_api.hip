@@ -308,13 +308,17 @@ int polykv_pages_accept(const polykv_pages* pages, const int32_t* tokens_dev, co
             set_error("%s: all arrays but counts must be given, 4-byte aligned", who);
             return POLYKV_EINVAL;
         }
-    const void* in[] = {tokens_dev, following_dev, parents_dev, counts_dev, pages->lengths_dev};
-    for (const void* p : in)
-        for (const void* q : {(const void*)path_dev, (const void*)accepted_dev, (const void*)next_dev, (const void*)kept_dev})
-            if (p == q) {   // (every layer's workgroups read the inputs)
-                set_error("%s: an output must not be an input", who);
-                return POLYKV_EINVAL;
-            }
+    const void* in[] = {tokens_dev, following_dev, parents_dev, counts_dev, pages->lengths_dev, pages->table_dev};
+    const void* out[] = {path_dev, accepted_dev, next_dev, kept_dev};
+    bool own = true;
+    for (const void*& q : out) {
+        for (const void* p : in) own &= p != q;   // (every layer's workgroups read the inputs)
+        for (const void*& p : out) own &= &p == &q || p != q;
+    }
+    if (!own) {
+        set_error("%s: an output must not be an input or another output", who);
+        return POLYKV_EINVAL;
+    }
     if (!aligned(counts_dev, 4)) {
         set_error("%s: counts must be 4-byte aligned", who);
         return POLYKV_EINVAL;

@@ -212,3 +212,13 @@ def test_out_that_overlaps_the_queries():
     for k in (0, nbytes):                  # (in place, and side by side: the workspace is what is refused)
         assert lib.pool_attend_tree(None, d, at(0), at(k), p, None) == pk.ENOMEM
         assert lib.pool_attend_tree(None, d, at(k), at(0), p, None) == pk.ENOMEM
+
+
+def test_accept_outputs_are_arrays_of_their_own():
+    table = C.c_void_p(0x60000)
+    d = C.byref(desc(table_dev=table))
+    out = [C.c_void_p(0x30000 + 0x1000 * k) for k in range(4)]
+    for k in range(4):
+        for x in (*[out[j] for j in range(4) if j != k], table):
+            args = [x if i == k else y for i, y in enumerate(out)]
+            assert lib.polykv_pages_accept(d, P, P, P, P, 4, *args, None) == pk.EINVAL
