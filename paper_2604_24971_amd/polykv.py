@@ -500,7 +500,7 @@ class Pages:
         device = torch.device(device)
         if device.type != "cuda":
             raise TypeError("pages lie in GPU memory, not on %s" % device)
-        self.device = torch.device(device.type, device.index if device.index is not None else 0)
+        self.device = torch.device(device.type, device.index if device.index is not None else torch.cuda.current_device())
         shape = (layers, pages, kv_heads, page_tokens, head_dim)
         self.K = torch.empty(shape, dtype=dtype, device=self.device)
         self.V = torch.empty(shape, dtype=dtype, device=self.device)

@@ -222,3 +222,21 @@ def test_accept_outputs_are_arrays_of_their_own():
         for x in (*[out[j] for j in range(4) if j != k], table):
             args = [x if i == k else y for i, y in enumerate(out)]
             assert lib.polykv_pages_accept(d, P, P, P, P, 4, *args, None) == pk.EINVAL
+
+
+def test_pages_on_the_current_device(monkeypatch):
+    """A device without a number is the current one, as it is for every tensor."""
+    torch = pytest.importorskip("torch")
+
+    class Asked(Exception):
+        pass
+
+    def empty(*_args, device=None, **_kw):
+        raise Asked(device)
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch, "empty", empty)
+    for device, index in (("cuda", 3), ("cuda:1", 1)):
+        with pytest.raises(Asked) as e:
+            pk.Pages(1, 2, 64, 4, 3, 2, page_tokens=8, device=device)
+        assert e.value.args[0] == torch.device("cuda", index)
