@@ -304,7 +304,8 @@ typedef struct {
  * updated.  slots_dev (NULL: not wanted) receives the places of the tokens that the agents grew by, agent after agent:
  * entry offsets[a] + i belongs to token (old length) + i of agent a and is page * page_tokens + token % page_tokens;
  * entries behind the last one are -1.  If there are more than `slots` tokens, those past that have no entry.
- * offsets_dev (NULL: not wanted): int32 [agents + 1]. */
+ * offsets_dev (NULL: not wanted): int32 [agents + 1].  Keys and values that are written by these slots have to be packed by these offsets,
+ * that is, without the rows of agents that did not grow. */
 int polykv_pages_resize(const polykv_pages* pages, const int32_t* targets_dev, int32_t* slots_dev, int slots,
                         int32_t* offsets_dev, void* stream);
 
@@ -340,7 +341,9 @@ typedef struct {
     int kernel;       /* of the pool's part                                                           */
     int splits;       /* token-range splits of the pool's part                                        */
     int key_precision;
-    int page_splits;  /* token-range splits of the pages' part; 0 = choose automatically              */
+    int page_splits;  /* token-range splits of the pages' part; 0 = choose automatically, for continuations
+                         as long as the block tables are wide (max_blocks).  Where they are much shorter, 1
+                         saves the partials and the launch that joins them                            */
     const int32_t* counts_dev;  /* [agents] drafts of each agent; NULL: `nodes`, as far as its length goes      */
     const uint64_t* mask_dev;   /* [agents, nodes, ceil(nodes / 64)]: the drafts that a draft sees, any set of
                                    them; NULL: itself and all before it                                         */
@@ -357,7 +360,10 @@ size_t pool_attend_tree_workspace(const polykv_pool* pool, const polykv_pages* p
  * attend the pool alone; a row that sees nothing gets zeros.  The pool's head_dim, layers and kv_heads must be the pages'.
  * A token that a draft does not see has no effect on it, whatever its vectors hold; a draft that sees a drafted token
  * with a NaN or infinite value gets NaN.  As in pool_attend, matrix-core kernels round probabilities to fp16 (two bfloat16
- * terms for bfloat16 pages), and bfloat16 queries of a call with a pool must stay below 65504. */
+ * terms for bfloat16 pages), and bfloat16 queries of a call with a pool must stay below 65504.
+ * Sizes: agents * nodes * (q_heads / kv_heads) <= 2^20, with or without a pool (262,140 if `kernel` is the vector kernel or int8 values
+ * at head_dim 256 choose it); layers of the range * kv_heads * agents * page_splits * row blocks (16 to 128 of an agent's nodes * q_heads /
+ * kv_heads rows are one) less than 2.13e9. */
 int pool_attend_tree(const polykv_pool* pool, const polykv_pages* pages, const void* Q_dev, void* out_dev,
                      const polykv_tree_params* params, void* stream);
 

@@ -55,9 +55,11 @@ __device__ __forceinline__ AgentChange change_of(const PageView& v, const int32_
 // written before they are done: the workgroup that is the last to say so writes the lengths and the ring's state (nobody waits
 // for anybody; a launch of its own for them took 4.5 us).  Pages that are given back go behind the ring's last, where no page to
 // be taken lies, so the two do not have to wait for each other.
-// A step of few agents is all latency: 256 threads there (15 agents that grow by 16 tokens each: 3.4 us at the fastest, with 1,024
-// threads 4.4).  1,024 agents that grow by up to 600 tokens take 9.3 us, and 6.1 to shrink: the four rounds of sums in front of
-// everything, then one round of stores.
+// A step of few agents is all latency: 256 threads there (15 agents: 3.0 us if nothing changes, 3.7 to grow by 16 tokens each, 5.3 with
+// their slots -- the bisection, then the ring or the table behind it --, 3.6 to shrink; with 1,024 threads about a microsecond more).
+// 1,024 agents are one round of sums, the chain of two scans by shuffles, two loops over the waves' sums and four barriers: 5.8 us of the
+// launch if nothing changes, 6.4 with the table entries of 600 new tokens each, 9.3 with their 460,000 slots, 6.1 to shrink.
+// 4,096 agents are four rounds: 17.2 us whatever is done behind them.
 // BY_AGENT: the slot map has per_agent.d entries for every agent and the third output is how far each grew, for callers whose rows
 // have places by agent: an agent that got nothing then moves nobody else's slots.
 template <int THREADS, bool BY_AGENT>

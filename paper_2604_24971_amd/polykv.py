@@ -525,7 +525,8 @@ class Pages:
         """Agent a's continuation becomes targets[a] tokens long: pages are taken for it or given back.  An agent for which
         there are no pages, or whose target is out of range, keeps its length.  `slots` (int32, any length) receives the
         places of the tokens that agents grew by, for write(), agent after agent, and -1 behind them; `offsets` (int32
-        [agents + 1]) where each agent's begin.
+        [agents + 1]) where each agent's begin: rows for write() are packed by them, without those of agents that kept their
+        length.
 
         With `granted` (int32 [agents]) places go by agent: `slots` is [agents, n], entry [a, i] the place of the i-th token
         that agent a grew by and -1 behind them, and granted[a] receives how many these are.  For rows of drafts [agents, n]
@@ -584,7 +585,9 @@ class Pages:
         them and the drafts that a draft's mask names.  Q [layers of the range, agents, nodes, q_heads, head_dim] of the
         pages' dtype; the result has its shape and dtype.  counts int32 [agents] (None: `nodes` for every agent); mask int64
         [agents, nodes, ceil(nodes / 64)] as tree_masks() makes it (None: a draft sees itself and all before it).  Rows
-        of drafts that an agent does not have see no private token."""
+        of drafts that an agent does not have see no private token.  `out` may be Q.  page_splits: token ranges of an agent;
+        by itself the call takes as many as continuations that fill the block tables need, and 1 is faster where they are much
+        shorter."""
         return self._attend_tree(None, Q, out, **kw)
 
     def _attend_tree(self, pool, Q, out, *, counts=None, mask=None, layer_begin=0, layer_end=None, scale=None, kernel=KERNEL_AUTO,
