@@ -219,7 +219,10 @@ template <int D, int R> struct Rows {
     }
 };
 
-// Scores -> probabilities in the pages' type, in operand order.  bfloat16's eight bits leave too much out: a second term holds it.
+// Scores -> probabilities in the pages' type, in operand order.  fp16: one term, whose rounding (half a step, 2^-11 of a weight, 2^-25
+// below the normal range) is as fine as the output's own; the denominator sums the rounded weights, so that what a weight loses
+// it loses on both sides of the fraction (errors 2.7e-4 of the output's rms, 2.1e-4 with weights in fp32; a second term would
+// double the value products).  bfloat16's eight bits leave too much out: a second term holds it.
 template <bool BF, int R> struct Weights {
     tree_uint4 p[R / 16], low[BF ? R / 16 : 1];
 };
