@@ -619,6 +619,8 @@ class Pages:
         # being captured gets one of its own from the graph's memory: graphs may be replayed on any streams.
         own = workspace is None
         capturing = own and _capturing(stream)
+        if not own and workspace.device != device:
+            raise ValueError("workspace is on %s, the pages on %s" % (workspace.device, device))
         ws = workspace if not own else None if capturing else self._workspaces.get(sp)
         if ws is not None:
             p.workspace_dev, p.workspace_bytes = ws.data_ptr() if own else _dev_ptr(ws, torch.uint8, "workspace"), ws.numel()

@@ -857,3 +857,13 @@ def test_in_place(d, nodes, group, layers, page_splits):
         both = Q.clone()
         assert call(both, both, page_splits=page_splits) is both
         assert torch.equal(both, want)
+
+
+def test_a_workspace_on_another_device():
+    """(The first of its places that the call may look at; one GPU is enough to see that.)"""
+    class Elsewhere:
+        device, is_cuda, dtype = torch.device("cuda", 1), True, torch.uint8
+
+    p = _pk().Pages(1, 2, 64, 4, 3, 2, page_tokens=8)
+    with pytest.raises(ValueError, match="workspace is on cuda:1"):
+        p.attend_tree(torch.zeros((1, 3, 2, 4, 64), dtype=F16, device="cuda"), workspace=Elsewhere())
