@@ -60,12 +60,12 @@ __device__ __forceinline__ AgentChange change_of(const PageView& v, const int32_
 // 1,024 agents are one round of sums, the chain of two scans by shuffles, two loops over the waves' sums and four barriers: 5.8 us of the
 // launch if nothing changes, 6.4 with the table entries of 600 new tokens each, 9.3 with their 460,000 slots, 6.1 to shrink.
 // 4,096 agents are four rounds: 17.2 us whatever is done behind them.
-// BY_AGENT: the slot map has per_agent.d entries for every agent and the third output is how far each grew, for callers whose rows
+// BY_AGENT: the slot map has n_slots / A entries for every agent and the third output is how far each grew, for callers whose rows
 // have places by agent: an agent that got nothing then moves nobody else's slots.
 template <int THREADS, bool BY_AGENT>
 __global__ __launch_bounds__(THREADS) void pages_resize_kernel(PageView v, const int32_t* __restrict__ targets, int32_t* ring,
                                                                int32_t* state, int32_t* ticket, int32_t* __restrict__ slots, int n_slots,
-                                                               int32_t* __restrict__ offsets, FastDiv per_agent) {
+                                                               int32_t* __restrict__ offsets) {
     extern __shared__ int shared[];
     int* const end_s = shared;                 // where an agent's new tokens end in the slot map
     int* const len_s = shared + v.A;           // its length
@@ -148,6 +148,7 @@ __global__ __launch_bounds__(THREADS) void pages_resize_kernel(PageView v, const
         const int b = v.div_P.divide(t, off);
         return b < have ? v.table[(size_t)a * v.max_blocks + b] : ring[(first + (uint32_t)at_s[a] + (uint32_t)(b - have)) % NP];
     };
+    [[maybe_unused]] const uint32_t per_agent = BY_AGENT ? (uint32_t)n_slots / (uint32_t)v.A : 0;
     // four slots of a thread
     for (int i0 = 4 * (blockIdx.x * THREADS + tid); i0 < n_slots; i0 += 4 * gridDim.x * THREADS) {
         int a = 0;
@@ -167,7 +168,7 @@ __global__ __launch_bounds__(THREADS) void pages_resize_kernel(PageView v, const
             if constexpr (BY_AGENT) {
                 if (i >= n_slots) continue;
                 int k;
-                a = per_agent.divide(i, &k);
+                a = i / per_agent, k = i - a * per_agent;
                 if (k < tgt_s[a] - len_s[a]) page[u] = page_of(a, len_s[a] + k, &off[u]);
             } else {
                 if (i >= grown) continue;
@@ -204,10 +205,9 @@ __global__ __launch_bounds__(THREADS) void pages_resize_kernel(PageView v, const
 }
 
 template <bool BY_AGENT>
-static hipError_t launch_resize(const polykv_pages* p, const int32_t* targets, int32_t* slots, int n_slots, int32_t* offsets, int per_agent,
+static hipError_t launch_resize(const polykv_pages* p, const int32_t* targets, int32_t* slots, int n_slots, int32_t* offsets,
                                 hipStream_t s) {
     const PageView v = page_view(p);
-    const FastDiv div = FastDiv::by(std::max(per_agent, 1));
     const int shared = 4 * v.A * (int)sizeof(int);
     if (shared > 48 * 1024) {   // (by call: the attribute belongs to the current device)
         const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(pages_resize_kernel<1024, BY_AGENT>), hipFuncAttributeMaxDynamicSharedMemorySize, shared);
@@ -216,22 +216,22 @@ static hipError_t launch_resize(const polykv_pages* p, const int32_t* targets, i
     if (slots == nullptr) n_slots = 0;
     if (v.A <= 64 && n_slots <= 4096) {
         launch_kernel(pages_resize_kernel<256, BY_AGENT>, dim3(1), dim3(256), shared, s, {}, v, targets, p->free_dev, p->free_state_dev, p->ticket_dev, slots,
-                      n_slots, offsets, div);
+                      n_slots, offsets);
     } else {
         const int by_slots = (n_slots + 4095) / 4096, by_agents = (v.A + 15) / 16;   // a round each: four slots a thread, an agent a wave
         launch_kernel(pages_resize_kernel<1024, BY_AGENT>, dim3(std::min(std::max(by_slots, by_agents), 256)), dim3(1024), shared, s, {}, v, targets, p->free_dev,
-                      p->free_state_dev, p->ticket_dev, slots, n_slots, offsets, div);
+                      p->free_state_dev, p->ticket_dev, slots, n_slots, offsets);
     }
     return hipGetLastError();
 }
 
 hipError_t launch_pages_resize(const polykv_pages* p, const int32_t* targets, int32_t* slots, int n_slots, int32_t* offsets,
                                hipStream_t s) {
-    return launch_resize<false>(p, targets, slots, n_slots, offsets, 0, s);
+    return launch_resize<false>(p, targets, slots, n_slots, offsets, s);
 }
 hipError_t launch_pages_resize_by_agent(const polykv_pages* p, const int32_t* targets, int32_t* slots, int per_agent, int32_t* granted,
                                         hipStream_t s) {
-    return launch_resize<true>(p, targets, slots, p->agents * per_agent, granted, per_agent, s);
+    return launch_resize<true>(p, targets, slots, p->agents * per_agent, granted, s);
 }
 
 // -------------------------------------------------------------------------------------- write ---
